@@ -340,6 +340,119 @@ int tabed_ensemble_step_static(const float* logits, const float* w, const float*
                                void* stream, int32_t* y, float* q, float* qk);
 int tabed_static_last_error(int32_t device, void* stream);
 
+/* ---- Paged caches in 8 bits -----------------------------------------------------------------------------
+ *
+ * Keys and values of many sequences in pages of page_tokens tokens: what the drafting inputs of a request, the branches of a
+ * token tree and requests that come and go share and give back, at one byte a value.  The caller owns every array (as with the
+ * weights of a handle); a tabed_pages only describes them, on one device and one stream, and no call allocates or
+ * synchronises (tabed_pages_last_error does).  Two calls on the same caches or the same workspace must not overlap on the GPU:
+ * one stream, or events.
+ *
+ * A value is code * scale: the code is e4m3 (4 bits of precision, at most 448 in size, no infinities), the scale belongs to a
+ * page, layer and KV head, K and V each their own.  tabed_pages_append and tabed_pages_compact choose scales 2^e, so that
+ * bringing codes to another scale is exact (but for values below 2^-6 of the new scale); the attention takes any positive one.
+ *
+ * `err` is a word on the device, zero at first, in which the calls record what they find in arrays that only the device sees;
+ * what such an entry asked for is not done, other entries of the call are.  tabed_pages_last_error names it:
+ *   TABED_ERR_INVALID_ARG   a sequence, page or index out of range, an entry's sequence named twice, or tokens to be written to a page that
+ *                           is not the sequence's own (ref other than 1: fork first)
+ *   TABED_ERR_KV_OVERFLOW   a position beyond max_pages * page_tokens, or no free page left
+ *   TABED_ERR_NUMERIC       tabed_pages_append met a value that is not finite (NaN is stored as 0, infinities as +-448 scale)
+ *   TABED_ERR_TIMEOUT       a bounded wait ran out */
+typedef struct {
+  void *k, *v;                 /* e4m3 codes [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], 16-byte aligned */
+  float *k_scale, *v_scale;    /* [n_layers][n_pages][n_kv_heads], > 0 */
+  int32_t *table;              /* [n_seqs][max_pages]: the page of every block of page_tokens tokens, -1 = none */
+  int32_t *ref;                /* [n_pages]: entries of `table` that name the page; 0 = free */
+  int32_t *err;                /* [1] */
+  void *workspace;             /* tabed_pages_workspace bytes, 16-byte aligned; contents need not be kept between calls */
+  int32_t n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_seqs, max_pages;
+                               /* page_tokens 16, 32, 64 or 128; head_dim 32, 64 or 128; n_seqs <= 32767 */
+  int32_t device;
+  void *stream;                /* cudaStream_t; NULL = legacy default stream */
+} tabed_pages;
+
+/* Bytes of workspace that the calls on caches of these sizes may use (a function of the sizes alone). */
+int tabed_pages_workspace(const tabed_pages* p, size_t* bytes);
+
+/* Copy, fork, cut, grow and free sequences: for each of n entries, sequence dst becomes the first keep tokens of sequence src,
+ * with room for len >= keep tokens.  The pages that the kept tokens fill are shared; where keep ends inside a page, dst gets a
+ * page of its own with copies of those tokens and of the scales, in all layers (src == dst: the page itself, if nobody else names it).  Blocks up to len get
+ * free pages, the lowest-numbered ones in the order of (entry, block); entries of dst's table beyond are -1, and the pages that
+ * it named before are given back.  src == dst grows (keep = the tokens it holds) or cuts a sequence, keep = len = 0 frees it.
+ * All entries see tables and caches as they were before the call, and pages given back by it are free for it.  An entry that
+ * runs out of pages has -1 in their place (KV_OVERFLOW).
+ * src, dst, keep, len: int32 [n], n <= n_seqs, every dst once.  Every block of src's kept tokens must have a page (INVALID_ARG). */
+int tabed_pages_fork(const tabed_pages* p, const int32_t* src, const int32_t* dst, const int32_t* keep, const int32_t* len, int32_t n);
+
+/* New tokens of one layer. */
+typedef struct {
+  int32_t layer;
+  int32_t n;                   /* entries: sequences that get tokens */
+  int32_t n_tokens, max_new;   /* rows of k, v (and q); no entry has more than max_new of them */
+  const int32_t *seq;          /* [n] sequence of an entry, every one at most once (NULL: entry i is sequence i) */
+  const int32_t *first;        /* [n + 1] entry i has the rows first[i] .. first[i + 1] - 1 */
+  const int32_t *start;        /* [n] position of its first token in the sequence */
+  int32_t dtype;               /* TABED_DTYPE_* of k, v, q and q_out */
+  const void *k, *v;           /* [n_tokens][n_kv_heads][head_dim], rows kv_stride elements apart (both) */
+  int64_t kv_stride;
+  int32_t n_axes;              /* 0: nothing is rotated (the other fields are ignored); else 1 .. 4 axes of positions */
+  int32_t sections[4];         /* frequencies that each axis drives, in order; their sum is head_dim / 2 */
+  const int32_t *positions;    /* [n_axes][n_tokens] */
+  float theta;                 /* > 0 */
+  const void *q;               /* [n_tokens][n_heads][head_dim], rows q_stride elements apart; NULL: keys alone */
+  void *q_out;                 /* the rotated queries, rows q_out_stride elements apart; may be q itself */
+  int32_t n_heads;
+  int64_t q_stride, q_out_stride;
+} tabed_pages_new;
+
+/* Rotates (n_axes > 0), rounds and writes new K and V, and rotates the queries that go with them.  Frequency i of head_dim / 2
+ * turns the pair (i, i + head_dim / 2) by positions[axis of i][token] * theta^(-2 i / head_dim): one axis for text, several
+ * (time, height, width) for image and video prefixes.  A block's scale becomes the least 2^e (-126 <= e <= 120) with
+ * |value| <= 448 * 2^e for all of its new tokens; where older tokens precede them in the block, at least the scale that it had, to which
+ * their codes are brought too.  Codes are rounded once from the fp32 rotation, to nearest even.  Tokens behind the new ones in their block are not kept.
+ * The blocks must have pages of their own (tabed_pages_fork). */
+int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t);
+
+/* Queries over one layer. */
+typedef struct {
+  int32_t layer;
+  int32_t n;                   /* entries */
+  int32_t n_tokens, max_new;   /* rows of q; no entry has more than max_new of them (more: INVALID_ARG, zeros) */
+  const int32_t *seq;          /* [n] sequence of an entry (NULL: entry i is sequence i); a sequence may be named by several */
+  const int32_t *first;        /* [n + 1] entry i has the rows first[i] .. first[i + 1] - 1 */
+  const int32_t *length;       /* [n] tokens in the sequence, those of the rows themselves (its last ones) included */
+  int32_t dtype;               /* TABED_DTYPE_* of q and out */
+  int32_t n_heads;             /* a multiple of n_kv_heads */
+  const void *q;               /* [n_tokens][n_heads][head_dim], rows q_stride elements apart */
+  void *out;                   /* the same, rows out_stride elements apart */
+  int64_t q_stride, out_stride;
+  float scale;                 /* > 0, of the products q k */
+  float softcap;               /* 0, or the cap c: scores become c tanh(score / c) */
+  const float *slopes;         /* [n_heads] or NULL: slope * |distance of the positions| is taken off the scores */
+  const int32_t *prefix;       /* [n] or NULL: the sequence's first tokens that every row sees, whatever its position */
+  const uint64_t *tree;        /* [n_tokens] or NULL: of its entry's r <= 64 rows, bit j says whether this row sees row j
+                                  (and not those before it); not with slopes */
+} tabed_pages_query;
+
+/* out = softmax(scores) V over the tokens that a row sees: row i of r sees the positions up to its own, length - r + i, and the
+ * prefix; with a tree the length - r positions before the rows, the prefix, and the rows of its mask.  A row that sees nothing is 0.
+ * Pages beyond the length and positions that no row of an entry sees may hold anything; a code that is NaN at a position that
+ * some rows of an entry see may reach others of its rows too (tabed_pages_append writes none).  A block without a page counts as not seen (INVALID_ARG).
+ * Rows of no entry are left as they are. */
+int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t);
+
+/* Keep some tokens of sequences and move them together (a token tree's accepted sibling behind its chain, pruned image tokens),
+ * in all layers: token start[i] + j becomes token index[i][j], j < count[i] <= width, ascending with index[i][j] >= start[i] + j.
+ * A block's scale becomes the largest of the scales that come together in it (the one it had where older tokens stay in it).
+ * The blocks written must be the sequence's own.  seq, start, count int32 [n] (every sequence at most once), index int32
+ * [n][width].  Tokens behind the moved ones are not kept in the last block written and otherwise left; tabed_pages_fork (src == dst) frees them. */
+int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t* start, const int32_t* count, const int32_t* index,
+                        int32_t n, int32_t width);
+
+/* Synchronises the stream, returns the code of what the calls recorded in `err` since the last time (TABED_OK if nothing), and clears it. */
+int tabed_pages_last_error(const tabed_pages* p);
+
 /* Stand-alone run of the tensor-core projection used for many shared-weight rows (Sec. 4.1 "batched
  * inference": all rows share the parameters, so a projection is one weights x rows contraction):
  * out[s][o] = sum_k w[o][k] * bf16(act[s][k]), fp32 accumulation.  w bf16 [rows][K], act float [n][K],

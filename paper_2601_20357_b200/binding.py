@@ -37,6 +37,8 @@ EXPORTS = [
     "tabed_select_path", "tabed_current_path", "tabed_debug_trace", "tabed_debug_gemm_tc",
     "tabed_last_device_error", "tabed_sync_lengths", "tabed_debug_barrier_timeout", "tabed_static_last_error",
     "tabed_set_policy_uniforms",
+    "tabed_pages_workspace", "tabed_pages_fork", "tabed_pages_append", "tabed_pages_attention", "tabed_pages_compact",
+    "tabed_pages_last_error",
 ]
 
 
@@ -53,6 +55,25 @@ class TabedConfig(C.Structure):
                [(n, C.c_int32) for n in ("n_inputs", "n_requests", "gamma", "window_h", "policy", "distance", "sample_mode")] + \
                [("tau", C.c_float), ("kv_capacity", C.c_int32), ("device", C.c_int32), ("stream", C.c_void_p),
                 ("tree_width", C.c_int32)]
+
+
+class TabedPages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "ref", "err", "workspace")] + \
+               [(n, C.c_int32) for n in ("n_layers", "n_pages", "n_kv_heads", "page_tokens", "head_dim", "n_seqs", "max_pages", "device")] + \
+               [("stream", C.c_void_p)]
+
+
+class TabedPagesNew(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "n", "n_tokens", "max_new")] + [(n, C.c_void_p) for n in ("seq", "first", "start")] + \
+               [("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("kv_stride", C.c_int64), ("n_axes", C.c_int32),
+                ("sections", C.c_int32 * 4), ("positions", C.c_void_p), ("theta", C.c_float), ("q", C.c_void_p), ("q_out", C.c_void_p),
+                ("n_heads", C.c_int32), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64)]
+
+
+class TabedPagesQuery(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "n", "n_tokens", "max_new")] + [(n, C.c_void_p) for n in ("seq", "first", "length")] + \
+               [("dtype", C.c_int32), ("n_heads", C.c_int32), ("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix", C.c_void_p), ("tree", C.c_void_p)]
 
 
 _PP = C.POINTER(C.c_void_p)
@@ -113,6 +134,13 @@ def lib() -> C.CDLL:
         L.tabed_sync_lengths.argtypes = [vp]
         L.tabed_debug_barrier_timeout.argtypes = [vp]
         L.tabed_static_last_error.argtypes = [i32, vp]
+        pages = C.POINTER(TabedPages)
+        L.tabed_pages_workspace.argtypes = [pages, C.POINTER(sz)]
+        L.tabed_pages_fork.argtypes = [pages, vp, vp, vp, vp, i32]
+        L.tabed_pages_append.argtypes = [pages, C.POINTER(TabedPagesNew)]
+        L.tabed_pages_attention.argtypes = [pages, C.POINTER(TabedPagesQuery)]
+        L.tabed_pages_compact.argtypes = [pages, vp, vp, vp, vp, i32, i32]
+        L.tabed_pages_last_error.argtypes = [pages]
         L.tabed_launch_count.argtypes = [vp]
         L.tabed_launch_count.restype = C.c_int64
         for name in EXPORTS:
@@ -350,6 +378,146 @@ class Tabed:
 
     def launch_count(self) -> int:
         return int(lib().tabed_launch_count(self._h))
+
+
+def _rows(t: torch.Tensor, dtype, n: int, heads: int, hd: int, name: str, device: torch.device) -> int:
+    """Pointer of rows [n][heads][hd] that are whole in themselves (stride(0) apart)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (n, heads, hd):
+        raise ValueError(f"{name}: expected shape {(n, heads, hd)}, got {tuple(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd) or (n > 1 and t.stride(0) < heads * hd):
+        raise ValueError(f"{name}: heads and values of a row must be contiguous, rows must not overlap")
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    return t.data_ptr()
+
+
+def _stride(t: torch.Tensor) -> int:
+    """Elements between rows; of one row, its length."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+_PAGES_DTYPE = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+
+
+class Pages:
+    """A paged cache in 8 bits over the caller's tensors (tabed_pages); method names follow the C entry points
+    (tabed_pages_<name>).
+
+    k, v: float8_e4m3fn (or uint8) [layers][pages][kv_heads][page_tokens][head_dim]; k_scale, v_scale: float32
+    [layers][pages][kv_heads]; table: int32 [sequences][blocks], -1 = none; ref: int32 [pages], 0 = free.  err (int32 [1], zero) and
+    workspace (uint8, `workspace_bytes`) are allocated here unless given; a workspace may be shared by caches whose calls do not
+    overlap on the GPU.  Calls run on `stream` (None: the legacy default stream) and allocate nothing."""
+
+    def __init__(self, *, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor,
+                 ref: torch.Tensor, err: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+        dev = k.device
+        if dev.type != "cuda":
+            raise ValueError(f"k: expected a CUDA device, got {dev}")
+        if k.dim() != 5 or table.dim() != 2:
+            raise ValueError("k: expected [layers][pages][kv_heads][page_tokens][head_dim], table: [sequences][blocks]")
+        if k.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise TypeError(f"k: expected torch.float8_e4m3fn or torch.uint8, got {k.dtype}")
+        L, NP, Hkv, ps, hd = k.shape
+        self.device, self.Hkv, self.hd, self.n_seqs = dev, Hkv, hd, table.shape[0]
+        p = TabedPages()
+        p.n_layers, p.n_pages, p.n_kv_heads, p.page_tokens, p.head_dim = L, NP, Hkv, ps, hd
+        p.n_seqs, p.max_pages = table.shape
+        p.device = dev.index if dev.index is not None else 0
+        p.stream = stream.cuda_stream if stream is not None else None
+        p.k, p.v = _ptr(k, k.dtype, None, "k", dev), _ptr(v, k.dtype, k.numel(), "v", dev)
+        p.k_scale = _ptr(k_scale, torch.float32, L * NP * Hkv, "k_scale", dev)
+        p.v_scale = _ptr(v_scale, torch.float32, L * NP * Hkv, "v_scale", dev)
+        p.table, p.ref = _ptr(table, torch.int32, None, "table", dev), _ptr(ref, torch.int32, NP, "ref", dev)
+        need = C.c_size_t()
+        _check(lib().tabed_pages_workspace(C.byref(p), C.byref(need)), "tabed_pages_workspace")
+        self.workspace_bytes = need.value
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=dev)
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        if workspace.numel() * workspace.element_size() < need.value:
+            raise ValueError(f"workspace: expected {need.value} bytes at least")
+        p.err, p.workspace = _ptr(err, torch.int32, 1, "err", dev), _ptr(workspace, workspace.dtype, None, "workspace", dev)
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.ref, self.err, self.workspace = k, v, k_scale, v_scale, table, ref, err, workspace
+        self._stream = stream
+        self._p = p
+        self._ref = C.byref(p)
+
+    def _entries(self, seq: Optional[torch.Tensor], first: torch.Tensor) -> int:
+        n = first.numel() - 1
+        if n < 0:
+            raise ValueError("first: expected at least one element")
+        if seq is None and n > self.n_seqs:
+            raise ValueError(f"first: {n} entries and {self.n_seqs} sequences")
+        return n
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor, keep: torch.Tensor, length: torch.Tensor) -> None:
+        n, d, i = src.numel(), self.device, torch.int32
+        _check(lib().tabed_pages_fork(self._ref, _ptr(src, i, n, "src", d), _ptr(dst, i, n, "dst", d), _ptr(keep, i, n, "keep", d),
+                                      _ptr(length, i, n, "length", d), n), "tabed_pages_fork")
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seq: Optional[torch.Tensor], first: torch.Tensor, start: torch.Tensor,
+               max_new: int, *, positions: Optional[torch.Tensor] = None, sections: Sequence[int] = (), theta: float = 10000.0,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
+        """k, v [tokens][kv_heads][head_dim] (rows may be views of wider ones, equally far apart); positions [axes][tokens] with
+        one of `sections` an axis: rotate k, and q into q_out where given."""
+        d, i, T, n = self.device, torch.int32, k.shape[0], self._entries(seq, first)
+        if k.dtype not in _PAGES_DTYPE:
+            raise TypeError(f"k: expected torch.float32 or torch.bfloat16, got {k.dtype}")
+        t = TabedPagesNew()
+        t.layer, t.n, t.n_tokens, t.max_new, t.dtype = layer, n, T, max_new, _PAGES_DTYPE[k.dtype]
+        t.seq, t.first, t.start = _ptr(seq, i, n, "seq", d), _ptr(first, i, n + 1, "first", d), _ptr(start, i, n, "start", d)
+        t.k, t.v, t.kv_stride = _rows(k, k.dtype, T, self.Hkv, self.hd, "k", d), _rows(v, k.dtype, T, self.Hkv, self.hd, "v", d), _stride(k)
+        if _stride(v) != t.kv_stride:
+            raise ValueError("v: rows must be as far apart as those of k")
+        if positions is not None:
+            t.n_axes = len(sections)
+            if not 1 <= t.n_axes <= 4:
+                raise ValueError("sections: expected 1 to 4 of them")
+            for a, x in enumerate(sections):
+                t.sections[a] = x
+            t.positions, t.theta = _ptr(positions, i, t.n_axes * T, "positions", d), theta
+        if q is not None:
+            if positions is None or q_out is None:
+                raise ValueError("q: needs positions and q_out")
+            H = q.shape[1]
+            t.q, t.q_out, t.n_heads = _rows(q, k.dtype, T, H, self.hd, "q", d), _rows(q_out, k.dtype, T, H, self.hd, "q_out", d), H
+            t.q_stride, t.q_out_stride = _stride(q), _stride(q_out)
+        _check(lib().tabed_pages_append(self._ref, C.byref(t)), "tabed_pages_append")
+
+    def attention(self, layer: int, q: torch.Tensor, out: torch.Tensor, seq: Optional[torch.Tensor], first: torch.Tensor, length: torch.Tensor,
+                  max_new: int, *, scale: float, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                  prefix: Optional[torch.Tensor] = None, tree: Optional[torch.Tensor] = None) -> None:
+        """q, out [tokens][heads][head_dim]; tree: int64 (or uint64) [tokens], the bits of the rows that a row sees."""
+        d, i, T, n = self.device, torch.int32, q.shape[0], self._entries(seq, first)
+        if q.dtype not in _PAGES_DTYPE:
+            raise TypeError(f"q: expected torch.float32 or torch.bfloat16, got {q.dtype}")
+        H = q.shape[1]
+        t = TabedPagesQuery()
+        t.layer, t.n, t.n_tokens, t.max_new, t.dtype, t.n_heads = layer, n, T, max_new, _PAGES_DTYPE[q.dtype], H
+        t.seq, t.first, t.length = _ptr(seq, i, n, "seq", d), _ptr(first, i, n + 1, "first", d), _ptr(length, i, n, "length", d)
+        t.q, t.q_stride = _rows(q, q.dtype, T, H, self.hd, "q", d), _stride(q)
+        t.out, t.out_stride = _rows(out, q.dtype, T, H, self.hd, "out", d), _stride(out)
+        t.scale, t.softcap = scale, softcap
+        t.slopes, t.prefix = _ptr(slopes, torch.float32, H, "slopes", d), _ptr(prefix, i, n, "prefix", d)
+        if tree is not None:
+            t.tree = _ptr(tree, tree.dtype if tree.dtype in (torch.int64, torch.uint64) else torch.int64, T, "tree", d)
+        _check(lib().tabed_pages_attention(self._ref, C.byref(t)), "tabed_pages_attention")
+
+    def compact(self, seq: torch.Tensor, start: torch.Tensor, count: torch.Tensor, index: torch.Tensor) -> None:
+        """index [entries][width]"""
+        n, d, i = seq.numel(), self.device, torch.int32
+        if index.dim() != 2 or index.shape[0] != n:
+            raise ValueError("index: expected [entries][width]")
+        _check(lib().tabed_pages_compact(self._ref, _ptr(seq, i, n, "seq", d), _ptr(start, i, n, "start", d), _ptr(count, i, n, "count", d),
+                                         _ptr(index, i, index.numel(), "index", d), n, index.shape[1]), "tabed_pages_compact")
+
+    def last_error(self) -> int:
+        """Code of what the calls recorded on the device since the last time (0 if nothing); clears the record."""
+        return int(lib().tabed_pages_last_error(self._ref))
 
 
 def weights_to_device(drafter, weights_np: Dict[str, object], device: torch.device) -> Dict[str, object]:

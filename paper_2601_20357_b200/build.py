@@ -8,8 +8,8 @@ import sys
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libtabed_b200.so")
-SOURCES = ["tabed.cu"]
-HEADERS = ["exact_math.cuh", "forward_kernels.cuh", "decide_kernels.cuh", "round_kernel.cuh", "proj_plan.h", "gemm_tc.cuh", "proj_tc.cuh", "attn_tc.cuh", "prompt_attn.cuh", "request_kernels.cuh", os.path.join("..", "..", "include", "tabed.h")]
+SOURCES = ["tabed.cu", "pages.cu"]
+HEADERS = ["ptx.cuh", "exact_math.cuh", "forward_kernels.cuh", "decide_kernels.cuh", "round_kernel.cuh", "proj_plan.h", "gemm_tc.cuh", "proj_tc.cuh", "attn_tc.cuh", "prompt_attn.cuh", "request_kernels.cuh", "pages_kernels.cuh", "pages_attn.cuh", os.path.join("..", "..", "include", "tabed.h")]
 
 
 def _stale() -> bool:
@@ -25,17 +25,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-shared", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo",
-           "-gencode", "arch=compute_100a,code=sm_100a",
-           "-o", LIB_PATH] + [os.path.join(CSRC, s) for s in SOURCES]
+    flags = ["-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a"]
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        flags += ["-Xptxas", "-v"]
+    objects = [os.path.join(CSRC, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+    runs = [subprocess.Popen([nvcc, "-c"] + flags + ["-o", o, os.path.join(CSRC, s)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            for s, o in zip(SOURCES, objects)]
+    said = [r.communicate()[0] for r in runs]
+    if all(r.returncode == 0 for r in runs):
+        link = subprocess.run([nvcc, "-shared"] + flags[-2:] + ["-o", LIB_PATH] + objects, capture_output=True, text=True)
+        runs, said = runs + [link], said + [link.stdout + link.stderr]
+    if any(r.returncode != 0 for r in runs):
+        raise RuntimeError("nvcc failed:\n" + "".join(said))
     if verbose:
-        sys.stderr.write(res.stderr)
+        sys.stderr.write("".join(said))
     return LIB_PATH
 
 

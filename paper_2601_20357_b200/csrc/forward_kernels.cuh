@@ -11,6 +11,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ptx.cuh"
+
 namespace tabed {
 
 struct SlotDesc { int row; int pos; int active; int pad; };
@@ -19,14 +21,6 @@ struct SlotDesc { int row; int pos; int active; int pad; };
 // element helpers
 // ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
-
-// Programmatic dependent launch (kernels of a chain launched with the stream-serialization attribute):
-// pdl_trigger lets the next kernel of the stream be scheduled while this one still runs; pdl_wait blocks
-// until every kernel before this one has completed and its writes are visible.  A kernel must not touch
-// memory that other kernels write, or that they may still read, before pdl_wait.  Both are no-ops in a
-// kernel launched without the attribute.
-__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {

@@ -20,7 +20,7 @@
 #include <stdint.h>
 
 #include "proj_plan.h"
-#include "round_kernel.cuh"   // PTX wrappers: mbarrier, bulk copy
+#include "round_kernel.cuh"
 
 namespace tabed {
 

@@ -1,0 +1,280 @@
+// C boundary of the paged 8-bit caches.  See include/tabed.h for the contract of every entry point; the kernels live in
+// pages_kernels.cuh / pages_attn.cuh.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "../../include/tabed.h"
+#include "pages_attn.cuh"
+#include "pages_kernels.cuh"
+
+using namespace tabed;
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr int kMaxPageSeqs = 32767;       // references and pins share a word of `ref` while a fork runs
+
+struct OnDevice {
+  int prev = -1; bool ok = true;
+  explicit OnDevice(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
+    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+  }
+  ~OnDevice() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int check(const tabed_pages* p) {
+  if (!p) return TABED_ERR_NULL_PTR;
+  if (!p->k || !p->v || !p->k_scale || !p->v_scale || !p->table || !p->ref || !p->err || !p->workspace) return TABED_ERR_NULL_PTR;
+  if (p->n_layers < 1 || p->n_pages < 1 || p->n_kv_heads < 1 || p->n_seqs < 1 || p->n_seqs > kMaxPageSeqs || p->max_pages < 1 ||
+      (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128) ||
+      (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) || p->device < 0 || p->device >= kMaxDevices ||
+      (long long)p->max_pages * p->page_tokens > 0x7FFFFF00ll || (long long)p->n_seqs * p->max_pages > 0x7FFFFFFFll || p->n_kv_heads > 1024 || p->n_layers > 32767)
+    return TABED_ERR_INVALID_ARG;
+  if (!aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->workspace, 16)) return TABED_ERR_INVALID_ARG;
+  return TABED_OK;
+}
+
+PagesDev on_device(const tabed_pages* p) {
+  PagesDev d;
+  d.k = static_cast<uint8_t*>(p->k); d.v = static_cast<uint8_t*>(p->v);
+  d.k_scale = p->k_scale; d.v_scale = p->v_scale; d.table = p->table; d.ref = p->ref; d.err = p->err;
+  d.L = p->n_layers; d.NP = p->n_pages; d.Hkv = p->n_kv_heads; d.ps = p->page_tokens; d.hd = p->head_dim;
+  d.n_seqs = p->n_seqs; d.max_pages = p->max_pages;
+  return d;
+}
+
+size_t round16(size_t x) { return (x + 15) & ~size_t(15); }
+
+// the fork's scratch: entries, counters, the kept blocks of every entry, the free pages
+size_t fork_free_pages(const tabed_pages* p) { return std::min((size_t)p->n_pages, (size_t)p->n_seqs * p->max_pages); }
+size_t fork_bytes(const tabed_pages* p) {
+  return round16((size_t)p->n_seqs * sizeof(ForkEntry)) + 16 + round16((size_t)p->n_seqs * p->max_pages * 4) + round16(fork_free_pages(p) * 4);
+}
+// the attention's: partial results of the segments at both ends of a CTA's part, their maxima and sums, what they belong to
+size_t attn_part_bytes(const tabed_pages* p) { return (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * p->head_dim * 4; }
+size_t attn_bytes(const tabed_pages* p) {
+  return attn_part_bytes(p) + (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * 2 * 4 + (size_t)kPgaMaxCtas * 2 * sizeof(int4);
+}
+
+// As a programmatic dependent of the kernel before it in the stream: every kernel here waits before it touches memory.
+template <typename ArgT>
+int launch(const tabed_pages* p, void (*kern)(ArgT), dim3 grid, int block, size_t smem, const ArgT& args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = reinterpret_cast<cudaStream_t>(p->stream);
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kern, args) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+  return TABED_OK;
+}
+
+int sm_count(int dev) {
+  static int n[kMaxDevices] = {0};
+  if (n[dev] == 0) {
+    int v = 0;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1) { cudaGetLastError(); return 148; }
+    n[dev] = v;
+  }
+  return n[dev];
+}
+
+// rows of `heads` heads of `hd` values of `esz` bytes, `stride` values apart, start on 16-byte boundaries
+bool rows_aligned(const void* p, long long stride, size_t esz) { return aligned(p, 16) && (stride * (long long)esz) % 16 == 0; }
+
+template <typename T>
+int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, bool small, size_t smem) {
+  if (small) return launch(p, k_pages_append<T, 32, 2>, grid, kAppendThreads, smem, a);
+  auto kern = k_pages_append<T, kAppendThreads, 4>;
+  static bool set[kMaxDevices] = {false};
+  if (!set[p->device]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 64 * (int)sizeof(float2)) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+    set[p->device] = true;
+  }
+  return launch(p, kern, grid, kAppendThreads, smem, a);
+}
+
+template <int HD, bool TWO, bool R8>
+int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
+  auto kern = k_pages_attn<HD, TWO, R8>;
+  static int per_sm[kMaxDevices] = {0};
+  if (per_sm[p->device] == 0) {
+    int n = 0;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pga_smem<HD>()) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kPgaThreads, pga_smem<HD>()) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      return TABED_ERR_CUDA;
+    }
+    per_sm[p->device] = n;
+  }
+  const int ctas = std::min(kPgaMaxCtas, per_sm[p->device] * sm_count(p->device));
+  const int rc = launch(p, kern, dim3(ctas), kPgaThreads, pga_smem<HD>(), a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas), 256, 0, a);
+}
+
+template <int HD>
+int launch_attn_hd(const tabed_pages* p, const PagesAttnArgs& a, bool f32) {
+  if (a.RB == 8) return f32 ? launch_attn<HD, true, true>(p, a) : launch_attn<HD, false, true>(p, a);
+  return f32 ? launch_attn<HD, true, false>(p, a) : launch_attn<HD, false, false>(p, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tabed_pages_workspace(const tabed_pages* p, size_t* bytes) {
+  if (!p || !bytes) return TABED_ERR_NULL_PTR;
+  if (p->n_pages < 1 || p->n_seqs < 1 || p->max_pages < 1 || p->head_dim < 1) return TABED_ERR_INVALID_ARG;
+  *bytes = std::max(fork_bytes(p), attn_bytes(p));
+  return TABED_OK;
+}
+
+int tabed_pages_fork(const tabed_pages* p, const int32_t* src, const int32_t* dst, const int32_t* keep, const int32_t* len, int32_t n) {
+  const int rc0 = check(p);
+  if (rc0 != TABED_OK) return rc0;
+  if (!src || !dst || !keep || !len) return TABED_ERR_NULL_PTR;
+  if (n < 0 || n > p->n_seqs) return TABED_ERR_INVALID_ARG;
+  if (n == 0) return TABED_OK;
+  OnDevice guard(p->device);
+  if (!guard.ok) return TABED_ERR_CUDA;
+  ForkArgs a;
+  a.P = on_device(p); a.n = n; a.src = src; a.dst = dst; a.keep = keep; a.len = len;
+  unsigned char* ws = static_cast<unsigned char*>(p->workspace);
+  a.ent = reinterpret_cast<ForkEntry*>(ws); ws += round16((size_t)p->n_seqs * sizeof(ForkEntry));
+  a.found = reinterpret_cast<int*>(ws); ws += 16;
+  a.rows = reinterpret_cast<int*>(ws); ws += round16((size_t)p->n_seqs * p->max_pages * 4);
+  a.free_list = reinterpret_cast<int*>(ws);
+  a.vec_ref = aligned(p->ref, 16);
+  int rc = launch(p, k_pages_share, dim3(n), kForkThreads, 0, a);
+  if (rc == TABED_OK) rc = launch(p, k_pages_alloc, dim3(1), kForkAllocThreads, 0, a);
+  if (rc == TABED_OK) rc = launch(p, k_pages_settle, dim3(n, 1 + 2 * p->n_layers), kForkThreads, 0, a);
+  return rc;
+}
+
+int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t) {
+  const int rc0 = check(p);
+  if (rc0 != TABED_OK) return rc0;
+  if (!t || !t->first || !t->start || !t->k || !t->v) return TABED_ERR_NULL_PTR;
+  const int hd = p->head_dim, half = hd / 2;
+  if (t->layer < 0 || t->layer >= p->n_layers || t->n < 0 || t->n > p->n_seqs || t->n_tokens < 0 || t->max_new < 0 ||
+      t->max_new > p->max_pages * p->page_tokens || (t->dtype != TABED_DTYPE_FP32 && t->dtype != TABED_DTYPE_BF16) ||
+      t->kv_stride < (long long)p->n_kv_heads * hd || t->n_axes < 0 || t->n_axes > 4)
+    return TABED_ERR_INVALID_ARG;
+  const bool with_q = t->n_axes > 0 && t->q;
+  const size_t esz = t->dtype == TABED_DTYPE_FP32 ? 4 : 2;
+  if (!aligned(t->k, esz) || !aligned(t->v, esz)) return TABED_ERR_INVALID_ARG;
+  if (t->n_axes > 0) {
+    if (!t->positions) return TABED_ERR_NULL_PTR;
+    if (!(t->theta > 0.0f) || !std::isfinite(t->theta)) return TABED_ERR_INVALID_ARG;
+    int sum = 0;
+    for (int i = 0; i < t->n_axes; ++i) { if (t->sections[i] < 0 || t->sections[i] > half) return TABED_ERR_INVALID_ARG; sum += t->sections[i]; }
+    if (sum != half) return TABED_ERR_INVALID_ARG;
+  }
+  if (with_q) {
+    if (!t->q_out) return TABED_ERR_NULL_PTR;
+    if (t->n_heads < 1 || t->n_heads > 4096 || t->q_stride < (long long)t->n_heads * hd || t->q_out_stride < (long long)t->n_heads * hd ||
+        !aligned(t->q, esz) || !aligned(t->q_out, esz))
+      return TABED_ERR_INVALID_ARG;
+  }
+  if (t->n == 0 || t->n_tokens == 0 || t->max_new == 0) return TABED_OK;
+  OnDevice guard(p->device);
+  if (!guard.ok) return TABED_ERR_CUDA;
+  AppendArgs a = {};
+  a.P = on_device(p); a.layer = t->layer; a.n = t->n; a.n_tokens = t->n_tokens; a.max_new = t->max_new; a.n_heads = t->n_heads;
+  a.seq = t->seq; a.first = t->first; a.start = t->start; a.positions = t->positions; a.k = t->k; a.v = t->v; a.q = t->q; a.q_out = t->q_out;
+  a.kv_stride = t->kv_stride; a.q_stride = t->q_stride; a.q_out_stride = t->q_out_stride; a.n_axes = t->n_axes; a.has_q = with_q;
+  a.vec_kv = rows_aligned(t->k, t->kv_stride, esz) && aligned(t->v, 16);
+  a.vec_q = with_q && rows_aligned(t->q, t->q_stride, esz) && rows_aligned(t->q_out, t->q_out_stride, esz);
+  for (int i = 0; i < t->n_axes; ++i) a.sections[i] = t->sections[i];
+  if (t->n_axes > 0)
+    for (int i = 0; i < half; ++i) a.turns[i] = pow((double)t->theta, -2.0 * i / hd) / 6.283185307179586476925;
+  const int ps = p->page_tokens, most = std::min(t->max_new, ps);      // tokens of a block
+  a.nblk = (t->max_new + ps - 2) / ps + 1;
+  // Units of a warp where a head's tokens of a block are at most 64 items of 8 pairs (a token of 128 values has 8 of them)
+  const bool small = most * (hd / 16) <= 64;
+  const int heads = 2 * p->n_kv_heads + (with_q ? t->n_heads : 0);
+  const long long blocks = (long long)t->n * a.nblk;
+  if (blocks > 0x7FFFFFFFll) return TABED_ERR_UNSUPPORTED;
+  // heads of a CTA: the cosines serve all of them, as long as the grid keeps some CTAs for every SM
+  const int per = small ? kAppendThreads / 32 : 1;
+  int groups = (int)std::min<long long>((heads + per - 1) / per, std::max<long long>(1, (8ll * sm_count(p->device) + blocks - 1) / blocks));
+  a.hpc = ((heads + groups - 1) / groups + per - 1) / per * per;
+  groups = (heads + a.hpc - 1) / a.hpc;
+  const size_t smem = t->n_axes > 0 ? (size_t)most * half * sizeof(float2) : 0;
+  const dim3 grid((unsigned)blocks, (unsigned)groups);
+  return t->dtype == TABED_DTYPE_FP32 ? launch_append<float>(p, a, grid, small, smem) : launch_append<__nv_bfloat16>(p, a, grid, small, smem);
+}
+
+int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {
+  const int rc0 = check(p);
+  if (rc0 != TABED_OK) return rc0;
+  if (!t || !t->first || !t->length || !t->q || !t->out) return TABED_ERR_NULL_PTR;
+  const int hd = p->head_dim;
+  const size_t esz = t->dtype == TABED_DTYPE_FP32 ? 4 : 2;
+  if (t->layer < 0 || t->layer >= p->n_layers || t->n < 0 || t->n_tokens < 0 || t->max_new < 0 ||
+      (t->dtype != TABED_DTYPE_FP32 && t->dtype != TABED_DTYPE_BF16) || t->n_heads < 1 || t->n_heads > 65536 || t->n_heads % p->n_kv_heads ||
+      t->q_stride < (long long)t->n_heads * hd || t->out_stride < (long long)t->n_heads * hd || !(t->scale > 0.0f) || !std::isfinite(t->scale) ||
+      !(t->softcap >= 0.0f) || !std::isfinite(t->softcap) || !aligned(t->q, esz) || !aligned(t->out, esz) || (t->tree && t->slopes) ||
+      (t->tree && t->max_new > 64) || !aligned(t->tree, 8))
+    return TABED_ERR_INVALID_ARG;
+  if (t->n == 0 || t->n_tokens == 0 || t->max_new == 0) return TABED_OK;
+  PagesAttnArgs a = {};
+  a.P = on_device(p); a.layer = t->layer; a.n = t->n; a.n_tokens = t->n_tokens; a.max_new = t->max_new; a.H = t->n_heads;
+  a.seq = t->seq; a.first = t->first; a.length = t->length; a.q = t->q; a.out = t->out; a.q_stride = t->q_stride; a.out_stride = t->out_stride;
+  a.scale = t->scale; a.softcap = t->softcap; a.slopes = t->slopes; a.prefix = t->prefix; a.tree = reinterpret_cast<const unsigned long long*>(t->tree);
+  a.vec_q = rows_aligned(t->q, t->q_stride, esz) && rows_aligned(t->out, t->out_stride, esz);
+  const long long rows = (long long)t->max_new * (t->n_heads / p->n_kv_heads);
+  a.WR = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+  a.RB = rows <= 8 ? 8 : 16 * a.WR;
+  // (an entry's chunks are counted in 31 bits, its rows too)
+  const long long tiles = ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) + a.RB - 1) / a.RB, chunks = ((long long)p->max_pages * p->page_tokens + 63) / 64;
+  if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFFF0ll || tiles * p->n_kv_heads > 0x7FFFFFFFll / chunks) return TABED_ERR_UNSUPPORTED;
+  unsigned char* ws = static_cast<unsigned char*>(p->workspace);
+  a.part = reinterpret_cast<float*>(ws); ws += attn_part_bytes(p);
+  a.part_ml = reinterpret_cast<float*>(ws); ws += (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * 2 * 4;
+  a.desc = reinterpret_cast<int4*>(ws);
+  OnDevice guard(p->device);
+  if (!guard.ok) return TABED_ERR_CUDA;
+  const bool f32 = t->dtype == TABED_DTYPE_FP32;
+  return hd == 32 ? launch_attn_hd<32>(p, a, f32) : (hd == 64 ? launch_attn_hd<64>(p, a, f32) : launch_attn_hd<128>(p, a, f32));
+}
+
+int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t* start, const int32_t* count, const int32_t* index,
+                        int32_t n, int32_t width) {
+  const int rc0 = check(p);
+  if (rc0 != TABED_OK) return rc0;
+  if (!seq || !start || !count || !index) return TABED_ERR_NULL_PTR;
+  if (n < 0 || n > p->n_seqs || width < 0) return TABED_ERR_INVALID_ARG;
+  if (n == 0 || width == 0) return TABED_OK;
+  OnDevice guard(p->device);
+  if (!guard.ok) return TABED_ERR_CUDA;
+  CompactArgs a;
+  a.P = on_device(p); a.seq = seq; a.start = start; a.count = count; a.index = index; a.n = n; a.width = width;
+  return launch(p, k_pages_compact, dim3(n, p->n_layers, 2 * p->n_kv_heads), kCompactThreads, 0, a);
+}
+
+int tabed_pages_last_error(const tabed_pages* p) {
+  if (!p || !p->err) return TABED_ERR_NULL_PTR;
+  if (p->device < 0 || p->device >= kMaxDevices) return TABED_ERR_INVALID_ARG;
+  OnDevice guard(p->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
+  int bits = 0;
+  if (!guard.ok || cudaMemcpyAsync(&bits, p->err, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaMemsetAsync(p->err, 0, sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+    cudaGetLastError();
+    return TABED_ERR_CUDA;
+  }
+  if (bits & (PERR_BARRIER | PERR_COPY)) return TABED_ERR_TIMEOUT;
+  if (bits & PGERR_INVALID) return TABED_ERR_INVALID_ARG;
+  if (bits & PERR_KV) return TABED_ERR_KV_OVERFLOW;
+  return bits & PGERR_NUMERIC ? TABED_ERR_NUMERIC : (bits ? TABED_ERR_CUDA : TABED_OK);
+}
+
+}  // extern "C"

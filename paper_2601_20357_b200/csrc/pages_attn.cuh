@@ -1,0 +1,596 @@
+// Attention over a paged 8-bit cache for few query rows a sequence: decoding steps, verified blocks, token trees.
+//
+//   out_i = sum_j softmax_j(s_ij) v_j,   s_ij = cap(scale q_i k_j) - slope |pos_i - j|,   k = codes * scale of their page
+//
+// The bytes of the cache bound it (2 hd bytes and 4 hd flops per position and query row), so:
+//   * the chunks (CH positions of one KV head) of all (entry, KV head, tile of rows) lie in one list, of which every CTA of a fixed grid
+//     walks a contiguous part of equal length: ragged batches and single long sequences split alike;
+//   * a producer warp looks pages up (32 blocks of the table at a time) and brings a chunk's pages into a ring of stages with one bulk copy
+//     per page, KV head and K or V, completing on an mbarrier; the scales travel beside them;
+//   * four consumer warps take the codes from shared memory as they lie (no swizzle: a row of codes is 32 - 128 bytes) and turn
+//     them into fp16 (exact) on the way into the fragments of mma.sync m16n8k16: scores with the query rows as A and positions as
+//     columns, whose accumulators are then the A fragments of P V.  The summed indices of both products (dims of q k, positions of P V) and the
+//     output columns are dealt so that a lane reads 4 - 16 neighbouring bytes: position pairs of V are interleaved with prmt;
+//   * a warp has 16 rows (8 of them live where there are no more) and a slice of the chunk, or a tile of rows of its own
+//     (WR = 1, 2 or 4 tiles of rows a CTA): with up to 16 rows the warps share them and meet at the end of a segment.
+// Numbers.  q is scaled by a power of two per row and rounded to fp16: exact for bf16 values; fp32 rows take a second term (22 bits).
+// With v's scale inside the exponent, w_j = 2^(s_j log2 e + log2 vs_j - M), the sum of w V needs no scale and the sum of
+// weights is that of w_j / vs_j.  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
+// M only moves when a score exceeds it by more than 2^3, so the sums are rarely rescaled.
+// Sequences that span CTAs are put together by k_pages_attn_join from the partial results, in fixed order.
+#pragma once
+#include "pages_kernels.cuh"
+
+namespace tabed {
+
+constexpr int kPgaWarps = 4;                     // consumers
+constexpr int kPgaThreads = 32 * (kPgaWarps + 1);
+constexpr int kPgaMaxCtas = 512;
+constexpr int kPgaMaxRows = 16 * kPgaWarps;      // query rows of a CTA
+template <int HD> __host__ __device__ constexpr int pga_chunk() { return HD == 128 ? 64 : 128; }
+template <int HD> __host__ __device__ constexpr int pga_stages() { return 4; }
+template <int HD> __host__ __device__ constexpr int pga_stage_bytes() { return 2 * pga_chunk<HD>() * HD; }
+template <int HD> __host__ __device__ constexpr size_t pga_smem() { return (size_t)pga_stages<HD>() * pga_stage_bytes<HD>() + (size_t)kPgaMaxRows * (HD + 2) * 4; }
+
+struct PagesAttnArgs {
+  PagesDev P;
+  int layer, n, n_tokens, max_new, H, WR, RB, vec_q;     // WR tiles of rows by warp; rows of a CTA: 16 WR, or 8
+  const int *seq, *first, *length;
+  const void* q;
+  void* out;
+  long long q_stride, out_stride;
+  float scale, softcap;
+  const float* slopes;
+  const int* prefix;
+  const unsigned long long* tree;
+  float* part;                        // [kPgaMaxCtas][2][rows][hd] partial outputs, then [..][rows][2] maxima and sums
+  float* part_ml;
+  int4* desc;                         // [kPgaMaxCtas][2] {valid | finished << 1, entry, KV head, tile of rows}
+};
+
+struct PgaEntry { int seq, q0, nq, len, bad; };
+
+// What an entry asks for, with its lengths brought into range; CTA 0 records `bad`.
+__device__ __forceinline__ PgaEntry pga_entry(const PagesAttnArgs& A, int e) {
+  PgaEntry E;
+  const int f0 = A.first[e], f1 = A.first[e + 1];
+  E.seq = A.seq ? A.seq[e] : e;
+  E.len = A.length[e];
+  E.bad = 0;
+  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens) { E.q0 = 0; E.nq = 0; E.bad = PGERR_INVALID; return E; }
+  E.q0 = f0; E.nq = f1 - f0;
+  if (E.seq < 0 || E.seq >= A.P.n_seqs || E.len < 0 || E.nq > A.max_new || (A.tree && E.nq > 64)) { E.seq = 0; E.len = 0; E.bad = PGERR_INVALID; }
+  if ((long long)E.len > (long long)A.P.max_pages * A.P.ps) { E.len = 0; E.bad = PERR_KV; }
+  return E;
+}
+
+struct PgaWalk { int e, kvh, rt, ch, nrt, nch; };      // entry, KV head, tile of rows, chunk; tiles, chunks of the entry
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// bounded wait of a warp; false if it ran out (recorded)
+__device__ __forceinline__ bool pga_wait(uint64_t* bar, unsigned parity, volatile int* dead, int* err) {
+  unsigned spins = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if (*dead) return false;
+    if (++spins > (1u << 20)) { atomicOr(err, PERR_COPY); *dead = 1; return false; }
+    if (spins > 4096) __nanosleep(64);
+  }
+  return true;
+}
+
+template <int N> struct PgaBytes;
+template <> struct PgaBytes<4> { uint32_t w[1]; __device__ __forceinline__ void load(const uint8_t* p) { w[0] = *reinterpret_cast<const uint32_t*>(p); } };
+template <> struct PgaBytes<8> { uint32_t w[2]; __device__ __forceinline__ void load(const uint8_t* p) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; } };
+template <> struct PgaBytes<16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const uint8_t* p) { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+};
+
+constexpr float kPgaFloor = -1e30f;              // the running maximum of a row that has seen nothing
+constexpr float kPgaSlack = 3.0f, kPgaLift = 12.0f;      // weights are at most 2^(slack + lift) = 2^15
+
+// TWO: fp32 rows (two fp16 terms of q and of the weights).  R8: no entry has more than 8 rows a KV head.
+template <int HD, bool TWO, bool R8>
+__global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs A) {
+  constexpr int CH = pga_chunk<HD>(), NS = pga_stages<HD>(), STAGE = pga_stage_bytes<HD>(), KS = HD / 16, NO = HD / 8;
+  constexpr int NG = HD == 128 ? 1 : 2, SB = 16 * NG;         // positions that a warp takes at once
+  constexpr unsigned FULL = 0xffffffffu;
+  extern __shared__ __align__(128) unsigned char pga_smem_raw[];
+  unsigned char* ring = pga_smem_raw;
+  float* so = reinterpret_cast<float*>(pga_smem_raw + NS * STAGE);        // [slices][rows][HD] states of the warps at a segment's end
+  float* sml = so + kPgaMaxRows * HD;                                      // [slices][rows][2]
+  __shared__ uint64_t full[NS], empty[NS];
+  __shared__ float4 meta[NS][CH / 16];           // of 16 positions: scale of k, log2 of v's scale, 1 / it
+  __shared__ long long s_part[kPgaThreads / 32], s_lo, s_hi;
+  __shared__ int s_e;
+  __shared__ long long s_off;
+  __shared__ int s_dead;
+  const PagesDev& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  const int H = A.H, Hkv = P.Hkv, grp = H / Hkv, ps = P.ps, WR = A.WR, WT = kPgaWarps / WR, RB = R8 ? 8 : 16 * WR;
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kPgaWarps); }
+    s_dead = 0; s_e = A.n;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_trigger();
+  pdl_wait();
+  if (tid < 2) A.desc[cta * 2 + tid] = make_int4(0, 0, 0, 0);
+  // chunks of an entry
+  auto shape = [&](const PgaEntry& E, PgaWalk& w) { w.nrt = (E.nq * grp + RB - 1) / RB; w.nch = max(1, (E.len + CH - 1) / CH); };
+  auto chunks_of = [&](int e) -> long long {
+    const PgaEntry E = pga_entry(A, e);
+    if (E.bad && cta == 0) atomicOr(P.err, E.bad);
+    PgaWalk w;
+    shape(E, w);
+    return (long long)Hkv * w.nrt * w.nch;
+  };
+  // the CTA's part of the list: every thread sums a strip of entries
+  const int per = (A.n + kPgaThreads - 1) / kPgaThreads, e0 = min(A.n, tid * per), e1 = min(A.n, e0 + per);
+  long long mine = 0, before;
+  for (int e = e0; e < e1; ++e) mine += chunks_of(e);
+  {
+    long long x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(FULL, x, o); if (lane >= o) x += y; }
+    if (lane == 31) s_part[warp] = x;
+    __syncthreads();
+    before = x - mine;
+    long long all = 0;
+    for (int w = 0; w < kPgaThreads / 32; ++w) { if (w < warp) before += s_part[w]; all += s_part[w]; }
+    const long long nc = all < gridDim.x ? all : gridDim.x;
+    const long long lo = cta < nc ? all * cta / nc : 0, hi = cta < nc ? all * (cta + 1) / nc : 0;
+    if (tid == 0) { s_lo = lo; s_hi = hi; }
+    if (lo < hi && before <= lo && lo < before + mine) {
+      long long at = before;
+      int e = e0;
+      for (;; ++e) { const long long c = chunks_of(e); if (lo < at + c) break; at += c; }
+      s_e = e; s_off = lo - at;
+    }
+  }
+  __syncthreads();
+  const int total = (int)(s_hi - s_lo);
+  if (total == 0) return;
+  PgaWalk w;
+  PgaEntry E;
+  auto seek = [&]() {
+    w.e = s_e;
+    E = pga_entry(A, w.e);
+    shape(E, w);
+    const int off = (int)s_off, item = off / w.nch;            // (an entry has fewer than 2^31 chunks: its positions and rows are 31 bits, checked by the host)
+    w.ch = off - item * w.nch; w.kvh = item / w.nrt; w.rt = item - w.kvh * w.nrt;
+  };
+  auto step = [&]() {                            // to the next chunk of the list
+    if (++w.ch < w.nch) return;
+    w.ch = 0;
+    if (++w.rt < w.nrt) return;
+    w.rt = 0;
+    if (++w.kvh < Hkv) return;
+    w.kvh = 0;
+    do { ++w.e; E = pga_entry(A, w.e); shape(E, w); } while (w.nrt == 0 && w.e + 1 < A.n);
+  };
+  seek();
+
+  if (warp == kPgaWarps) {
+    // ---- producer ----
+    int cb = -1, ce = -1, ck = -1;               // block that lane 0 has looked up, entry, KV head
+    int pg = -1;
+    float pks = 1.0f, pvs = 1.0f;
+    const int ppc = ps < CH ? CH / ps : 1;       // pages of a chunk
+    const int rows = ps < CH ? ps : CH;          // positions that it takes of each
+    bool ok = true;
+    int c = 0;
+    for (; c < total; ++c) {
+      const int st = c % NS;
+      if (c >= NS) { ok = pga_wait(&empty[st], (unsigned)(c / NS - 1) & 1u, &s_dead, P.err); ok = __all_sync(FULL, ok); if (!ok) break; }
+      const int p0 = w.ch * CH, blk0 = p0 / ps, nblk = (E.len + ps - 1) / ps;
+      if (w.e != ce || blk0 < cb || blk0 + ppc > cb + 32) {
+        cb = blk0; ce = w.e; ck = -1;
+        const int b = cb + lane;
+        pg = b < nblk ? P.table[(size_t)E.seq * P.max_pages + b] : -1;
+        if (b < nblk && (pg < 0 || pg >= P.NP)) { atomicOr(P.err, PGERR_INVALID); pg = -2; }
+      }
+      if (w.kvh != ck) {
+        ck = w.kvh;
+        if (pg >= 0) {
+          const size_t at = ((size_t)A.layer * P.NP + pg) * Hkv + w.kvh;
+          pks = P.k_scale[at]; pvs = P.v_scale[at];
+        }
+      }
+      const int mypg = __shfl_sync(FULL, pg, min(blk0 + lane - cb, 31) & 31);
+      const bool has = lane < ppc && blk0 + lane < nblk && mypg >= 0;
+      const unsigned bytes = (unsigned)rows * HD, n_has = __popc(__ballot_sync(FULL, has));
+      unsigned char* sk = ring + st * STAGE;
+      {
+        const int src = ((p0 + lane * 16) / ps - cb) & 31;       // (lanes beyond the chunk's groups read something and drop it)
+        const float ks = __shfl_sync(FULL, pks, src), vs = __shfl_sync(FULL, pvs, src);
+        const int gp = __shfl_sync(FULL, pg, src);
+        if (lane < CH / 16) {
+          const float lv = fmaxf(lg2_approx(vs), -126.0f);
+          meta[st][lane] = gp >= 0 ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        }
+      }
+      if (lane < ppc && blk0 + lane < nblk && mypg < 0) {       // no page: nothing there, and nothing stale either
+        for (unsigned i = 0; i < 2 * bytes; i += 16)
+          *reinterpret_cast<uint4*>(sk + (i < bytes ? lane * bytes + i : (unsigned)CH * HD + lane * bytes + i - bytes)) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      __syncwarp();
+      if (lane == 0) { if (n_has) mbar_expect_tx(&full[st], 2 * n_has * bytes); else mbar_arrive(&full[st]); }
+      __syncwarp();
+      if (has) {
+        const size_t at = (((size_t)A.layer * P.NP + mypg) * Hkv + w.kvh) * ps * HD + (size_t)(ps > CH ? p0 % ps : 0) * HD;
+        bulk_g2s(sk + lane * bytes, P.k + at, bytes, &full[st]);
+        bulk_g2s(sk + CH * HD + lane * bytes, P.v + at, bytes, &full[st]);
+      }
+      if (c + 1 < total) step();
+    }
+    if (lane == 0) {                             // the last copies land before the shared memory goes, whatever the consumers did
+      for (int i = max(0, c - NS); i < c; ++i) {
+        unsigned spins = 0;
+        while (!mbar_try_wait(&full[i % NS], (unsigned)(i / NS) & 1u) && ++spins < (1u << 16)) __nanosleep(64);
+      }
+    }
+    return;
+  }
+
+  // ---- consumers ----
+  const int g = lane >> 2, t = lane & 3, wr = warp % WR, wt = warp / WR, TS = CH / WT;
+  const int perm = (g & ~1) + ((g & 1) ^ ((g >> 1) & 1));      // position of column g among 8, and of a lane's two columns:
+  const int c0 = 2 * t + (t & 1), c1 = 2 * t + 1 - (t & 1);
+  const float log2e = 1.4426950408889634f;
+  const bool cap = A.softcap > 0.0f, slow = cap || A.slopes != nullptr;
+  uint32_t qf[TWO ? 2 : 1][KS][4];
+  float o[NO][4], M[2], l[2], cr[2], slope[2];
+  int lim[2], pos[2], lim_min = 0, lim_max = 0, base = 0;
+  unsigned long long bits[2] = {0, 0};
+  bool whole_from = false, live = true;
+  int nr = 0;
+
+  auto load_q = [&]() {
+    nr = E.nq * grp;
+    base = E.len - E.nq;
+    const int pre = A.prefix ? min(max(A.prefix[w.e], 0), E.len) : 0;
+    const int r_lo = w.rt * RB + wr * 16, r_hi = min(nr, r_lo + 16) - 1;
+    live = r_lo < nr;
+    // positions below `lim` are seen by a row (with a tree: and those of its mask)
+    auto limit = [&](int r) { return A.tree ? max(base, pre) : min(E.len, max(base + r / grp + 1, pre)); };
+    lim_min = live ? max(0, limit(r_lo)) : 0;
+    lim_max = !live ? 0 : (A.tree ? E.len : max(0, limit(r_hi)));
+#pragma unroll
+    for (int x = 0; x < (R8 ? 1 : 2); ++x) {
+      const int r = r_lo + g + 8 * x;
+      const bool there = r < nr;
+      const int i = there ? r / grp : 0, h = w.kvh * grp + (there ? r - i * grp : 0);
+      pos[x] = base + i;
+      lim[x] = there ? limit(r) : 0;
+      bits[x] = there && A.tree ? A.tree[E.q0 + i] : 0ull;
+      slope[x] = there && A.slopes ? A.slopes[h] * log2e : 0.0f;
+      float v[HD / 4];
+      const long long at = (long long)(E.q0 + i) * A.q_stride + (long long)h * HD;
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) {        // the dims of a lane: the 8 or 16 bytes of a row of codes that it reads
+        const int d = HD == 32 ? t * 8 : (k >> 1) * 64 + t * 16 + (k & 1) * 8;
+        float f[8];
+        if (!there) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+        } else if (TWO) load8(reinterpret_cast<const float*>(A.q) + at + d, A.vec_q, f);
+        else load8(reinterpret_cast<const __nv_bfloat16*>(A.q) + at + d, A.vec_q, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[k * 8 + j] = f[j];
+      }
+      float amax = 0.0f;
+#pragma unroll
+      for (int j = 0; j < HD / 4; ++j) amax = fmaxf(amax, fabsf(v[j]));
+      amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, 2));
+      // largest value of the row to 2^14 .. 2^15
+      const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
+      const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23), down = __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+      cr[x] = cap ? A.scale / A.softcap * down : A.scale * log2e * down;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const float a = v[4 * ks] * up, b = v[4 * ks + 1] * up, cc = v[4 * ks + 2] * up, d = v[4 * ks + 3] * up;
+        qf[0][ks][x] = pack_f16(a, b);
+        qf[0][ks][2 + x] = pack_f16(cc, d);
+        if (TWO) {
+          const float2 h0 = f16x2_to_float2(qf[0][ks][x]), h1 = f16x2_to_float2(qf[0][ks][2 + x]);
+          qf[TWO ? 1 : 0][ks][x] = pack_f16(a - h0.x, b - h0.y);
+          qf[TWO ? 1 : 0][ks][2 + x] = pack_f16(cc - h1.x, d - h1.y);
+        }
+      }
+      M[x] = kPgaFloor; l[x] = 0.0f;
+    }
+    if (R8) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) { qf[0][ks][1] = 0; qf[0][ks][3] = 0; if (TWO) { qf[TWO ? 1 : 0][ks][1] = 0; qf[TWO ? 1 : 0][ks][3] = 0; } }
+    }
+#pragma unroll
+    for (int i = 0; i < NO; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+  };
+
+  // SB positions from `j0` of the sequence, `in` of the chunk
+  auto attend = [&](const unsigned char* sk, const float4* mt, int in, int j0) {
+    constexpr int NX = R8 ? 2 : 4;
+    float s[NG][2][4];
+#pragma unroll
+    for (int gg = 0; gg < NG; ++gg)
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[gg][a][j] = 0.0f;
+        const unsigned char* row = sk + (in + 16 * gg + 8 * a + perm) * HD;
+#pragma unroll
+        for (int b = 0; b < (HD == 128 ? 2 : 1); ++b) {
+          PgaBytes<HD == 32 ? 8 : 16> kb;
+          kb.load(row + b * 64 + t * (HD == 32 ? 8 : 16));
+#pragma unroll
+          for (int k = 0; k < (HD == 32 ? 2 : 4); ++k) {
+            uint32_t b0, b1;
+            e4m3x4_to_f16x4(kb.w[k], b0, b1);
+            const int ks = b * 4 + k;
+            mma_f16(s[gg][a], qf[0][ks][0], qf[0][ks][1], qf[0][ks][2], qf[0][ks][3], b0, b1);
+            if (TWO) mma_f16(s[gg][a], qf[TWO ? 1 : 0][ks][0], qf[TWO ? 1 : 0][ks][1], qf[TWO ? 1 : 0][ks][2], qf[TWO ? 1 : 0][ks][3], b0, b1);
+          }
+        }
+      }
+    const bool edge = j0 + SB > lim_min;         // some row does not see all of these positions
+    // scores in base 2, v's scale included
+#pragma unroll
+    for (int gg = 0; gg < NG; ++gg) {
+      const float4 m = mt[(in >> 4) + gg];
+      if (!slow) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int j = 0; j < NX; ++j) s[gg][a][j] = fmaf(s[gg][a][j], cr[j >> 1] * m.x, m.y);
+      } else {
+        const int jg = j0 + 16 * gg;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int j = 0; j < NX; ++j) {
+            float z = s[gg][a][j] * (cr[j >> 1] * m.x);
+            if (cap) z = (A.softcap * log2e) * (1.0f - 2.0f * rcp_approx(1.0f + ex2_approx(z * (2.0f * log2e))));      // tanh
+            z -= slope[j >> 1] * fabsf((float)(pos[j >> 1] - (jg + 8 * a + ((j & 1) ? c1 : c0))));
+            s[gg][a][j] = z + m.y;
+          }
+      }
+    }
+    if (edge) {
+#pragma unroll
+      for (int gg = 0; gg < NG; ++gg)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int j = 0; j < NX; ++j) {
+            const int jp = j0 + 16 * gg + 8 * a + ((j & 1) ? c1 : c0), d = jp - base;
+            bool seen = jp < lim[j >> 1];
+            if (A.tree) seen = seen || (jp < E.len && d >= 0 && d < 64 && ((bits[j >> 1] >> (d & 63)) & 1ull));
+            if (!seen) s[gg][a][j] = -INFINITY;
+          }
+    }
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int gg = 0; gg < NG; ++gg)
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int j = 0; j < NX; ++j) top[j >> 1] = fmaxf(top[j >> 1], s[gg][a][j]);
+    const bool grow = top[0] > M[0] + kPgaSlack || (!R8 && top[1] > M[1] + kPgaSlack);
+    if (__any_sync(FULL, grow)) {
+#pragma unroll
+      for (int x = 0; x < (R8 ? 1 : 2); ++x) {
+        float n = top[x];
+        n = fmaxf(n, __shfl_xor_sync(FULL, n, 1));
+        n = fmaxf(n, __shfl_xor_sync(FULL, n, 2));
+        n = fmaxf(n, M[x]);
+        const float f = ex2_approx(M[x] - n);
+        M[x] = n; l[x] *= f;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) { o[i][2 * x] *= f; o[i][2 * x + 1] *= f; }
+      }
+    }
+#pragma unroll
+    for (int gg = 0; gg < NG; ++gg) {
+      const float inv = mt[(in >> 4) + gg].z;
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int j = 0; j < NX; ++j) {
+          const float p = ex2_approx(s[gg][a][j] - (M[j >> 1] - kPgaLift));
+          l[j >> 1] = fmaf(p, inv, l[j >> 1]);
+          s[gg][a][j] = p;
+        }
+      uint32_t ph[4], pl[4];
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (R8 && x == 1) { ph[2 * a + 1] = 0; pl[2 * a + 1] = 0; continue; }
+          ph[2 * a + x] = pack_f16(s[gg][a][2 * x], s[gg][a][2 * x + 1]);
+          if (TWO) {
+            const float2 h = f16x2_to_float2(ph[2 * a + x]);
+            pl[2 * a + x] = pack_f16(s[gg][a][2 * x] - h.x, s[gg][a][2 * x + 1] - h.y);
+          }
+        }
+      // the lane's four positions of V: pairs (c0, c1) of the group's two halves, NO neighbouring dims
+      const unsigned char* vr = sk + CH * HD + (in + 16 * gg) * HD + g * NO;
+      PgaBytes<NO> v[4];
+      v[0].load(vr + c0 * HD); v[1].load(vr + c1 * HD); v[2].load(vr + (8 + c0) * HD); v[3].load(vr + (8 + c1) * HD);
+      if (edge) {                                // what lies behind the last position seen may be anything, and 0 * NaN is not 0
+        const int jg = j0 + 16 * gg;
+        const uint32_t k0 = jg + c0 < lim_max ? ~0u : 0u, k1 = jg + c1 < lim_max ? ~0u : 0u, k2 = jg + 8 + c0 < lim_max ? ~0u : 0u, k3 = jg + 8 + c1 < lim_max ? ~0u : 0u;
+#pragma unroll
+        for (int i = 0; i < NO / 4; ++i) { v[0].w[i] &= k0; v[1].w[i] &= k1; v[2].w[i] &= k2; v[3].w[i] &= k3; }
+      }
+#pragma unroll
+      for (int i = 0; i < NO / 4; ++i) {
+        uint32_t b[4][2];
+        e4m3x4_to_f16x4(__byte_perm(v[0].w[i], v[1].w[i], 0x5140), b[0][0], b[1][0]);
+        e4m3x4_to_f16x4(__byte_perm(v[0].w[i], v[1].w[i], 0x7362), b[2][0], b[3][0]);
+        e4m3x4_to_f16x4(__byte_perm(v[2].w[i], v[3].w[i], 0x5140), b[0][1], b[1][1]);
+        e4m3x4_to_f16x4(__byte_perm(v[2].w[i], v[3].w[i], 0x7362), b[2][1], b[3][1]);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          mma_f16(o[4 * i + d], ph[0], ph[1], ph[2], ph[3], b[d][0], b[d][1]);
+          if (TWO) mma_f16(o[4 * i + d], pl[0], pl[1], pl[2], pl[3], b[d][0], b[d][1]);
+        }
+      }
+    }
+  };
+
+  // one row's dims d .. d + 3 of the result
+  auto put = [&](int r, int d, float4 v) {
+    const int i = r / grp, h = w.kvh * grp + r - i * grp;
+    const long long at = (long long)(E.q0 + i) * A.out_stride + (long long)h * HD + d;
+    if (TWO) {
+      float* p = reinterpret_cast<float*>(A.out) + at;
+      if (A.vec_q) *reinterpret_cast<float4*>(p) = v;
+      else { p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w; }
+    } else {
+      __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(A.out) + at;
+      if (A.vec_q) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      else { p[0] = __float2bfloat16_rn(v.x); p[1] = __float2bfloat16_rn(v.y); p[2] = __float2bfloat16_rn(v.z); p[3] = __float2bfloat16_rn(v.w); }
+    }
+  };
+
+  // The segment's states to shared memory; all consumers put them together and write the result or the part.
+  auto finish = [&](bool from_start, bool to_end) {
+    const int slices = WT;
+#pragma unroll
+    for (int x = 0; x < (R8 ? 1 : 2); ++x) {
+      float sum = l[x];
+      sum += __shfl_xor_sync(FULL, sum, 1);
+      sum += __shfl_xor_sync(FULL, sum, 2);
+      const int rr = wr * 16 + g + 8 * x;
+      if (w.rt * RB + rr < nr) {
+        float* p = so + ((size_t)wt * RB + rr) * HD + 2 * t * NO;
+#pragma unroll
+        for (int i = 0; i < NO; i += 4) {
+          *reinterpret_cast<float4*>(p + i) = make_float4(o[i][2 * x], o[i + 1][2 * x], o[i + 2][2 * x], o[i + 3][2 * x]);
+          *reinterpret_cast<float4*>(p + NO + i) = make_float4(o[i][2 * x + 1], o[i + 1][2 * x + 1], o[i + 2][2 * x + 1], o[i + 3][2 * x + 1]);
+        }
+        if (t == 0) *reinterpret_cast<float2*>(sml + ((size_t)wt * RB + rr) * 2) = make_float2(M[x], sum);
+      }
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kPgaWarps) : "memory");
+    const int rows = min(RB, nr - w.rt * RB);
+    const bool whole = from_start && to_end;
+    const int slot = cta * 2 + (from_start ? 1 : 0);
+    for (int x = tid; x < rows * (HD / 4); x += 32 * kPgaWarps) {
+      const int r = x / (HD / 4), d = (x - r * (HD / 4)) * 4;
+      float m = kPgaFloor, sum = 0.0f;
+      for (int k = 0; k < slices; ++k) m = fmaxf(m, sml[(k * RB + r) * 2]);
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int k = 0; k < slices; ++k) {
+        const float f = ex2_approx(sml[(k * RB + r) * 2] - m);
+        const float4 u = *reinterpret_cast<const float4*>(so + ((size_t)k * RB + r) * HD + d);
+        sum += sml[(k * RB + r) * 2 + 1] * f;
+        v.x += u.x * f; v.y += u.y * f; v.z += u.z * f; v.w += u.w * f;
+      }
+      if (whole) {
+        const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+        // (a sum that is not a number leaves its row that way)
+        const bool none = sum == 0.0f;
+        put(w.rt * RB + r, d, none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : (sum > 0.0f ? make_float4(v.x * f, v.y * f, v.z * f, v.w * f) : make_float4(sum, sum, sum, sum)));
+      } else {
+        *reinterpret_cast<float4*>(A.part + ((size_t)slot * kPgaMaxRows + r) * HD + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(A.part_ml + ((size_t)slot * kPgaMaxRows + r) * 2) = make_float2(m, sum);
+      }
+    }
+    if (!whole && tid == 0) A.desc[slot] = make_int4(1 | (to_end ? 2 : 0), w.e, w.kvh, w.rt);
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kPgaWarps) : "memory");
+  };
+
+  // (a wait that ran out is recorded, and all others then return at once: the warps meet at every segment's end, so they run through)
+  bool fresh = true;
+  for (int c = 0; c < total; ++c) {
+    const int st = c % NS;
+    if (fresh) { whole_from = w.ch == 0; load_q(); fresh = false; }
+    pga_wait(&full[st], (unsigned)(c / NS) & 1u, &s_dead, P.err);
+    __syncwarp();
+    const unsigned char* sk = ring + st * STAGE;
+    const int j0 = w.ch * CH + wt * TS;
+#pragma unroll 1
+    for (int i = 0; i < TS; i += SB)
+      if (j0 + i < lim_max) attend(sk, meta[st], wt * TS + i, j0 + i);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&empty[st]);
+    if (w.ch == w.nch - 1 || c == total - 1) { finish(whole_from, w.ch == w.nch - 1); fresh = true; }
+    if (c + 1 < total) step();
+  }
+}
+
+// Puts the parts of the items that span CTAs together: block c takes the item that begins in CTA c and goes on behind it.
+template <int HD, bool TWO>
+__global__ void __launch_bounds__(256) k_pages_attn_join(const PagesAttnArgs A) {
+  __shared__ int s_n;
+  const int c = blockIdx.x, tid = threadIdx.x, grp = A.H / A.P.Hkv, RB = A.RB;
+  pdl_trigger();
+  pdl_wait();
+  const int4 d = A.desc[c * 2 + 1];
+  if (!(d.x & 1)) return;
+  if (tid == 0) {                                // CTAs that have a part of it
+    int n = 1;
+    while (c + n < gridDim.x) { const int x = A.desc[(c + n) * 2].x; if (!(x & 1)) break; ++n; if (x & 2) break; }
+    s_n = n;
+  }
+  __syncthreads();
+  const int n = s_n, e = d.y, kvh = d.z, rt = d.w;
+  const PgaEntry E = pga_entry(A, e);
+  const int rows = min(RB, E.nq * grp - rt * RB);
+  auto slot = [&](int k) { return (size_t)(k == 0 ? c * 2 + 1 : (c + k) * 2) * kPgaMaxRows; };
+  for (int x = tid; x < rows * (HD / 4); x += blockDim.x) {
+    const int r = x / (HD / 4), dd = (x - r * (HD / 4)) * 4;
+    float m = kPgaFloor, sum = 0.0f;
+    for (int k = 0; k < n; ++k) m = fmaxf(m, A.part_ml[(slot(k) + r) * 2]);
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float2 ml = *reinterpret_cast<const float2*>(A.part_ml + (slot(k) + r) * 2);
+      const float4 u = *reinterpret_cast<const float4*>(A.part + (slot(k) + r) * HD + dd);
+      const float f = ex2_approx(ml.x - m);
+      sum += ml.y * f;
+      v.x += u.x * f; v.y += u.y * f; v.z += u.z * f; v.w += u.w * f;
+    }
+    const int row = rt * RB + r, i = row / grp, h = kvh * grp + row - i * grp;
+    const long long at = (long long)(E.q0 + i) * A.out_stride + (long long)h * HD + dd;
+    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+    v = sum == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : (sum > 0.0f ? make_float4(v.x * f, v.y * f, v.z * f, v.w * f) : make_float4(sum, sum, sum, sum));
+    if (TWO) {
+      float* p = reinterpret_cast<float*>(A.out) + at;
+      if (A.vec_q) *reinterpret_cast<float4*>(p) = v;
+      else { p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w; }
+    } else {
+      __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(A.out) + at;
+      if (A.vec_q) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      else { p[0] = __float2bfloat16_rn(v.x); p[1] = __float2bfloat16_rn(v.y); p[2] = __float2bfloat16_rn(v.z); p[3] = __float2bfloat16_rn(v.w); }
+    }
+  }
+}
+
+}  // namespace tabed

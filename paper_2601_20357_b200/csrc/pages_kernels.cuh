@@ -1,0 +1,556 @@
+// Paged 8-bit caches: the kernels that keep the pages (fork, compact) and write new tokens into them (append).  The
+// attention over them is in pages_attn.cuh.  Contracts: include/tabed.h.
+//
+// A cached value is an e4m3 code times the scale of its page, layer and KV head.  Scales written here are powers of two: bringing codes to a larger scale only
+// moves the exponent, so a page that fills up token by token holds, but for values that become subnormal, what one rounding
+// of every value would have given, and the 3 bits of mantissa lose nothing against a scale amax / 448.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ptx.cuh"
+
+namespace tabed {
+
+enum { PGERR_NUMERIC = 1, PGERR_INVALID = 32 };       // beside PERR_KV and PERR_COPY
+
+struct PagesDev {
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  int *table, *ref, *err;
+  int L, NP, Hkv, ps, hd, n_seqs, max_pages;
+};
+
+// ---- e4m3 ------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t v) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+  return r;
+}
+// four codes of a word: (0, 1) and (2, 3) as pairs of fp16 values (exact)
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {      // to nearest even, saturating
+  uint32_t r;
+  asm("{\n .reg .b16 x, y;\n cvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n mov.b32 %0, {x, y};\n}\n"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
+__device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
+// the codes of a word at `ratio` times their scale's inverse
+__device__ __forceinline__ uint32_t e4m3x4_rescale(uint32_t w, float ratio) {
+  uint32_t lo, hi;
+  e4m3x4_to_f16x4(w, lo, hi);
+  const float2 a = f16x2_to_float2(lo), b = f16x2_to_float2(hi);
+  return to_e4m3x4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio);
+}
+// the least 2^e, -126 <= e <= 120, with amax <= 448 * 2^e  (448 = 1.75 * 2^8)
+__device__ __forceinline__ float least_scale(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  e = min(max(e, -126), 120);
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// ---- append ----------------------------------------------------------------------------------------
+struct AppendArgs {
+  PagesDev P;
+  int layer, n, n_tokens, max_new, n_heads, nblk, hpc, n_axes, has_q;
+  const int *seq, *first, *start, *positions;
+  const void *k, *v, *q;
+  void* q_out;
+  long long kv_stride, q_stride, q_out_stride;
+  int vec_kv, vec_q;                  // rows start on 16-byte boundaries
+  int sections[4];
+  double turns[64];                   // theta^(-2 i / hd) / (2 pi)
+};
+
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool vec, float (&f)[8]) {
+  if (vec) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __bfloat162float(p[i]);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, bool vec, float (&f)[8]) {
+  if (vec) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = p[i];
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, bool vec, const float (&f)[8]) {
+  if (vec) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(f[i]);
+  }
+}
+__device__ __forceinline__ void store8(float* p, bool vec, const float (&f)[8]) {
+  if (vec) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = f[i];
+  }
+}
+
+// Whether another of the n entries names the sequence of entry e (all threads of the block take part; n_threads of them).
+__device__ __forceinline__ bool named_twice(const int* seq, int e, int n) {
+  int twice = 0;
+  const int s = seq[e];
+  for (int i = threadIdx.x; i < n; i += blockDim.x) twice |= (i != e && seq[i] == s);
+  return __syncthreads_or(twice) != 0;
+}
+
+constexpr int kAppendThreads = 256;
+
+// A CTA has one block of page_tokens tokens of one entry and hpc of the K, V and query heads: the cosines and sines of
+// its tokens are taken once (the angle's turns in fp64: positions of any size) and serve all of those heads.  A unit (a head's
+// tokens of the block) is worked by TPU threads, each with up to MAXI items of 8 rotated pairs in registers between the
+// block's maximum and the rounding: k, v and q are read once.  Short units (single tokens) take a warp each, 8 at once;
+// long ones the whole CTA.
+template <typename T, int TPU, int MAXI>
+__global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArgs A) {
+  extern __shared__ float2 ap_cs[];               // [tokens of the block][hd / 2] cosine, sine
+  __shared__ float s_red[kAppendThreads / 32];
+  const PagesDev& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int e = blockIdx.x / A.nblk, slot = blockIdx.x - e * A.nblk;
+  pdl_trigger();
+  pdl_wait();
+  const int s = A.seq ? A.seq[e] : e, f0 = A.first[e], f1 = A.first[e + 1], p0 = A.start[e], ps = P.ps, hd = P.hd, half = hd >> 1;
+  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens || s < 0 || s >= P.n_seqs || p0 < 0 || f1 - f0 > A.max_new) {
+    if (tid == 0) atomicOr(P.err, PGERR_INVALID);
+    return;
+  }
+  if ((long long)p0 + (f1 - f0) > (long long)P.max_pages * ps) {
+    if (tid == 0) atomicOr(P.err, PERR_KV);
+    return;
+  }
+  const int p1 = p0 + (f1 - f0), bi = p0 / ps + slot;
+  if (f1 == f0 || bi * ps >= p1) return;
+  const int lo = max(p0, bi * ps), cnt = min(p1, (bi + 1) * ps) - lo, off = lo - bi * ps, t0 = f0 + (lo - p0);
+  const int page = P.table[(size_t)s * P.max_pages + bi];
+  bool own = page >= 0 && page < P.NP;
+  if (own) own = P.ref[page] == 1;
+  const int u0 = blockIdx.y * A.hpc, u1 = min(u0 + A.hpc, 2 * P.Hkv + (A.has_q ? A.n_heads : 0));
+  if (A.n_axes) {
+    for (int i = tid; i < cnt * half; i += kAppendThreads) {
+      const int tok = i / half, f = i - tok * half;
+      int axis = 0, upto = A.sections[0];
+      while (f >= upto && axis < A.n_axes - 1) upto += A.sections[++axis];
+      double turn = (double)A.positions[(size_t)axis * A.n_tokens + t0 + tok] * A.turns[f];
+      turn -= rint(turn);
+      float sn, cs;
+      sincospif((float)(2.0 * turn), &sn, &cs);
+      ap_cs[i] = make_float2(cs, sn);
+    }
+  }
+  if (A.seq && named_twice(A.seq, e, A.n)) {      // (a barrier, too)
+    if (tid == 0) atomicOr(P.err, PGERR_INVALID);
+    return;
+  }
+  __syncthreads();
+  if (!own && tid == 0) atomicOr(P.err, PGERR_INVALID);
+  const int per_tok = hd >> 4, n_items = cnt * per_tok;
+  constexpr int UNITS = kAppendThreads / TPU;
+  const int me = TPU == 32 ? lane : tid;
+  for (int u = u0 + (TPU == 32 ? warp : 0); u < u1; u += UNITS) {
+    const bool is_q = u >= 2 * P.Hkv, is_v = !is_q && u >= P.Hkv;
+    if (!is_q && !own) continue;
+    const int head = is_q ? u - 2 * P.Hkv : (is_v ? u - P.Hkv : u);
+    const T* in = reinterpret_cast<const T*>(is_q ? A.q : (is_v ? A.v : A.k)) + (size_t)head * hd;
+    const long long stride = is_q ? A.q_stride : A.kv_stride;
+    const bool vec = is_q ? A.vec_q : A.vec_kv, turned = A.n_axes && !is_v;
+    float x[MAXI][16], amax = 0.0f;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < MAXI; ++j) {
+      const int it = me + j * TPU;
+      if (it >= n_items) break;
+      const int tok = it / per_tok, c = it - tok * per_tok;
+      const T* row = in + (long long)(t0 + tok) * stride + c * 8;
+      float a[8], b[8];
+      load8(row, vec, a);
+      load8(row + half, vec, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float y = a[i], z = b[i];
+        if (turned) {
+          const float2 cs = ap_cs[tok * half + c * 8 + i];
+          y = a[i] * cs.x - b[i] * cs.y;
+          z = b[i] * cs.x + a[i] * cs.y;
+        }
+        x[j][i] = y; x[j][8 + i] = z;
+      }
+      if (is_q) {
+        T* o = reinterpret_cast<T*>(A.q_out) + (size_t)head * hd + (long long)(t0 + tok) * A.q_out_stride + c * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { a[i] = x[j][i]; b[i] = x[j][8 + i]; }
+        store8(o, vec, a);
+        store8(o + half, vec, b);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float m = fabsf(x[j][i]);
+          if (m < INFINITY) amax = fmaxf(amax, m); else odd = true;
+        }
+      }
+    }
+    if (is_q) continue;
+    const size_t at = ((size_t)A.layer * P.NP + page) * P.Hkv + head;
+    float* scale = (is_v ? P.v_scale : P.k_scale) + at;
+    uint8_t* codes = (is_v ? P.v : P.k) + at * ps * hd;
+    const float old = off > 0 ? *scale : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (TPU > 32) {
+      if (lane == 0) s_red[warp] = amax;
+      __syncthreads();
+      amax = s_red[lane & 7];
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      __syncthreads();                            // (everybody has read the old scale, and the next unit may use s_red)
+    }
+    const float now = fmaxf(least_scale(amax), old), inv = 1.0f / now;
+    if (me == 0) *scale = now;
+    if (odd) atomicOr(P.err, PGERR_NUMERIC);
+    if (off > 0 && now != old) {
+      const float ratio = old / now;
+      for (int i = me; i < off * (hd >> 3); i += TPU) {
+        uint2* w = reinterpret_cast<uint2*>(codes) + i;
+        uint2 c = *w;
+        c.x = e4m3x4_rescale(c.x, ratio);
+        c.y = e4m3x4_rescale(c.y, ratio);
+        *w = c;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < MAXI; ++j) {
+      const int it = me + j * TPU;
+      if (it >= n_items) break;
+      const int tok = it / per_tok, c = it - tok * per_tok;
+      uint8_t* row = codes + (size_t)(off + tok) * hd + c * 8;
+      float y[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = x[j][i] != x[j][i] ? 0.0f : x[j][i] * inv;     // (the conversion saturates)
+      *reinterpret_cast<uint2*>(row) = make_uint2(to_e4m3x4(y[0], y[1], y[2], y[3]), to_e4m3x4(y[4], y[5], y[6], y[7]));
+      *reinterpret_cast<uint2*>(row + half) = make_uint2(to_e4m3x4(y[8], y[9], y[10], y[11]), to_e4m3x4(y[12], y[13], y[14], y[15]));
+    }
+  }
+}
+
+// ---- fork ------------------------------------------------------------------------------------------
+// Three launches: the references of the pages shared, pinned and given back (a CTA an entry; atomic additions, whose order does
+// not matter), the free pages (one CTA: who needs how many, and the lowest-numbered ones in order), the tables and the copies.
+// While the call runs a page's word in `ref` holds its references in the low half and in the high half how many entries copy from
+// it: such a page is not handed out even where nobody names it any longer.
+struct ForkEntry { int valid, stays, first_new, tail; };     // tail: page of the block that keep ends in, -1 if it ends with a block
+
+struct ForkArgs {
+  PagesDev P;
+  int n;
+  const int *src, *dst, *keep, *len;
+  ForkEntry* ent;                     // [n_seqs]
+  int* found;                         // [4]: free pages found
+  int* rows;                          // [n_seqs][max_pages] the kept blocks of an entry, as they were before the call
+  int* free_list;                     // [min(n_pages, n_seqs * max_pages)]
+  int vec_ref;                        // ref starts on a 16-byte boundary
+};
+
+constexpr int kForkThreads = 256;
+constexpr int kForkAllocThreads = 1024;
+
+__global__ void __launch_bounds__(kForkThreads) k_pages_share(const ForkArgs A) {
+  const PagesDev& P = A.P;
+  const int e = blockIdx.x, tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  const int src = A.src[e], dst = A.dst[e], keep = A.keep[e], len = A.len[e];
+  int bad = src < 0 || src >= P.n_seqs || dst < 0 || dst >= P.n_seqs || keep < 0 || len < keep;
+  const bool over = !bad && len > P.max_pages * P.ps;
+  bad |= over;
+  const int full = bad ? 0 : keep / P.ps, part = bad ? 0 : keep % P.ps;
+  const int* from = P.table + (size_t)(bad ? 0 : src) * P.max_pages;
+  int lost = 0;
+  for (int b = tid; b < full + (part > 0); b += kForkThreads) { const int pg = from[b]; lost |= pg < 0 || pg >= P.NP; }
+  bad |= __syncthreads_or(lost);
+  bad |= named_twice(A.dst, e, A.n);
+  if (tid == 0) {
+    A.ent[e] = ForkEntry{!bad, 0, 0, bad || part == 0 ? -1 : from[full]};
+    if (bad) atomicOr(P.err, over ? PERR_KV : PGERR_INVALID);
+  }
+  if (bad) return;
+  int* row = A.rows + (size_t)e * P.max_pages;
+  for (int b = tid; b < full; b += kForkThreads) {
+    const int pg = from[b];
+    row[b] = pg;
+    atomicAdd(P.ref + pg, 1);
+  }
+  if (tid == 0 && part > 0) atomicAdd(P.ref + from[full], 1 << 16);
+  const int* to = P.table + (size_t)dst * P.max_pages;
+  for (int b = tid; b < P.max_pages; b += kForkThreads) {
+    const int pg = to[b];
+    if (pg >= 0 && pg < P.NP) atomicAdd(P.ref + pg, -1);
+  }
+}
+
+// the sum of v over the threads before this one; *total over all (1024 threads; s_scan of 33 words)
+__device__ __forceinline__ int block_scan(int v, int* s_scan, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+  if (lane == 31) s_scan[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int w = s_scan[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += y; }
+    s_scan[lane] = w;
+  }
+  __syncthreads();
+  *total = s_scan[31];
+  const int before = (warp ? s_scan[warp - 1] : 0) + x - v;
+  __syncthreads();
+  return before;
+}
+
+__global__ void __launch_bounds__(kForkAllocThreads) k_pages_alloc(const ForkArgs A) {
+  __shared__ int s_scan[33];
+  const PagesDev& P = A.P;
+  const int tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  int need_all = 0;
+  for (int base = 0; base < A.n; base += kForkAllocThreads) {
+    const int e = base + tid;
+    int need = 0;
+    if (e < A.n && A.ent[e].valid) {
+      const int keep = A.keep[e], full = keep / P.ps, tail = A.ent[e].tail;
+      const int stays = tail >= 0 && A.src[e] == A.dst[e] && (P.ref[tail] & 0xFFFF) == 0;
+      need = (A.len[e] + P.ps - 1) / P.ps - full - stays;
+      A.ent[e].stays = stays;
+    }
+    int total;
+    const int before = block_scan(need, s_scan, &total);
+    if (e < A.n) A.ent[e].first_new = need_all + before;
+    need_all += total;
+  }
+  // (every decision above has been taken: the pages that stay with their sequence get their reference)
+  for (int e = tid; e < A.n; e += kForkAllocThreads)
+    if (A.ent[e].valid && A.ent[e].stays) atomicAdd(P.ref + A.ent[e].tail, 1);
+  __syncthreads();
+  constexpr int PER = 8;
+  int found = 0;
+  for (long long base = 0; base < P.NP && found < need_all; base += kForkAllocThreads * PER) {
+    const long long p0 = base + (long long)tid * PER;
+    int r[PER], mine = 0;
+    if (A.vec_ref && p0 + PER <= P.NP) {
+#pragma unroll
+      for (int j = 0; j < PER; j += 4) *reinterpret_cast<int4*>(r + j) = *reinterpret_cast<const int4*>(P.ref + p0 + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) r[j] = p0 + j < P.NP ? P.ref[p0 + j] : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) mine += r[j] == 0;
+    int total, at = found + block_scan(mine, s_scan, &total);
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (r[j] == 0) { if (at < need_all) A.free_list[at] = (int)(p0 + j); ++at; }
+    found += total;
+  }
+  if (tid == 0) {
+    A.found[0] = min(found, need_all);
+    if (found < need_all) atomicOr(P.err, PERR_KV);
+  }
+}
+
+// grid (n, 1 + 2 L): the table, then K and V of a layer
+__global__ void __launch_bounds__(kForkThreads) k_pages_settle(const ForkArgs A) {
+  const PagesDev& P = A.P;
+  const int e = blockIdx.x, tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  const ForkEntry E = A.ent[e];
+  if (!E.valid) return;
+  const int keep = A.keep[e], full = keep / P.ps, part = keep % P.ps, nb = (A.len[e] + P.ps - 1) / P.ps, kept = full + E.stays, found = A.found[0];
+  if (blockIdx.y == 0) {
+    int* to = P.table + (size_t)A.dst[e] * P.max_pages;
+    const int* row = A.rows + (size_t)e * P.max_pages;
+    for (int b = tid; b < P.max_pages; b += kForkThreads) {
+      int pg = -1;
+      if (b < full) pg = row[b];
+      else if (b < kept) pg = E.tail;
+      else if (b < nb) {
+        const int at = E.first_new + b - kept;
+        if (at < found) { pg = A.free_list[at]; P.ref[pg] = 1; }
+      }
+      to[b] = pg;
+    }
+    if (tid == 0 && E.tail >= 0) atomicAdd(P.ref + E.tail, -(1 << 16));
+    return;
+  }
+  if (E.tail < 0 || E.stays || E.first_new >= found) return;
+  const int page = A.free_list[E.first_new], layer = (blockIdx.y - 1) >> 1;
+  const bool is_v = (blockIdx.y - 1) & 1;
+  uint8_t* codes = is_v ? P.v : P.k;
+  float* scale = is_v ? P.v_scale : P.k_scale;
+  const size_t of = ((size_t)layer * P.NP + E.tail) * P.Hkv, at = ((size_t)layer * P.NP + page) * P.Hkv;
+  for (int i = tid; i < P.Hkv; i += kForkThreads) scale[at + i] = scale[of + i];
+  const int head_bytes = P.ps * P.hd, vecs = part * P.hd >> 4;          // 16-byte pieces of a head's kept tokens
+  for (int i = tid; i < P.Hkv * vecs; i += kForkThreads) {
+    const int h = i / vecs, x = (i - h * vecs) << 4;
+    *reinterpret_cast<uint4*>(codes + (at + h) * head_bytes + x) = *reinterpret_cast<const uint4*>(codes + (of + h) * head_bytes + x);
+  }
+}
+
+// ---- compact ---------------------------------------------------------------------------------------
+struct CompactArgs {
+  PagesDev P;
+  const int *seq, *start, *count, *index;
+  int n, width;
+};
+constexpr int kCompactThreads = 256;
+constexpr int kCompactTile = 1024;        // tokens whose places are looked up at once (a multiple of page_tokens)
+
+// A CTA has one entry, layer and KV head of K or V and fills the target blocks one by one.  Sources lie at or behind their
+// targets in ascending order, so no source of a block lies in a block filled before it; the reads of a block and its writes are
+// parted by the barriers of the scale's maximum, and the next block's reads are on their way meanwhile.
+// grid (n, L, 2 Hkv)
+__global__ void __launch_bounds__(kCompactThreads) k_pages_compact(const CompactArgs A) {
+  const PagesDev& P = A.P;
+  const int e = blockIdx.x, layer = blockIdx.y, head = blockIdx.z >> 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool is_v = blockIdx.z & 1;
+  __shared__ long long s_src[kCompactTile];     // a token's page * page_tokens + its place in the page
+  __shared__ float s_red[2][kCompactThreads / 32];
+  pdl_trigger();
+  pdl_wait();
+  const int s = A.seq[e], start = A.start[e], count = A.count[e], ps = P.ps, hd = P.hd, cap = P.max_pages * ps;
+  const int* index = A.index + (size_t)e * A.width;
+  int bad = s < 0 || s >= P.n_seqs || start < 0 || count < 0 || count > A.width || start > cap - count;
+  const int* table = P.table + (size_t)(bad ? 0 : s) * P.max_pages;
+  if (!bad) {
+    for (int i = tid; i < count; i += kCompactThreads) {
+      const int x = index[i];
+      int wrong = x < start + i || x >= cap || (i > 0 && index[i - 1] >= x);
+      if (!wrong) { const int pg = table[x / ps]; wrong = pg < 0 || pg >= P.NP; }
+      bad |= wrong;
+    }
+    if (count > 0)
+      for (int b = start / ps + tid; b <= (start + count - 1) / ps; b += kCompactThreads) {
+        const int pg = table[b];
+        bad |= pg < 0 || pg >= P.NP || P.ref[pg] != 1;
+      }
+  }
+  bad = __syncthreads_or(bad);
+  bad |= named_twice(A.seq, e, A.n);
+  if (bad) {
+    if (tid == 0) atomicOr(P.err, PGERR_INVALID);
+    return;
+  }
+  if (count == 0) return;
+  uint8_t* codes = (is_v ? P.v : P.k) + ((size_t)layer * P.NP * P.Hkv + head) * ps * hd;        // + page * Hkv * ps * hd
+  float* scale = (is_v ? P.v_scale : P.k_scale) + (size_t)layer * P.NP * P.Hkv + head;          // + page * Hkv
+  const size_t page_codes = (size_t)P.Hkv * ps * hd;
+  const int vec_tok = hd >> 4;
+  constexpr int MAXV = 4;                       // 16-byte pieces of a block per thread: 128 tokens of 128 bytes
+  uint4 now[MAXV], next[MAXV];
+  float now_s[MAXV], next_s[MAXV];
+  // first token (of the entry's moved ones), tokens and place of target block b
+  auto span = [&](int b, int& i0, int& cnt, int& off) {
+    const int lo = max(start, b * ps), hi = min(start + count, (b + 1) * ps);
+    i0 = lo - start; cnt = hi - lo; off = lo - b * ps;
+  };
+  int tile0 = 0;
+  auto look_up = [&](int i0) {                  // places of the tokens i0 .. of the next tile
+    tile0 = i0;
+    for (int i = tid; i < kCompactTile && i0 + i < count; i += kCompactThreads) {
+      const int x = index[i0 + i];
+      s_src[i] = (long long)table[x / ps] * ps + x % ps;
+    }
+    __syncthreads();
+  };
+  auto fetch = [&](int i0, int cnt, uint4 (&w)[MAXV], float (&ws)[MAXV]) {
+#pragma unroll
+    for (int j = 0; j < MAXV; ++j) {
+      const int x = tid + j * kCompactThreads;
+      ws[j] = 0.0f;
+      if (x < cnt * vec_tok) {
+        const int tok = x / vec_tok;
+        const long long at = s_src[i0 - tile0 + tok], page = at / ps, row = at - page * ps;
+        w[j] = *reinterpret_cast<const uint4*>(codes + page * page_codes + row * hd + ((x - tok * vec_tok) << 4));
+        ws[j] = scale[page * P.Hkv];
+      }
+    }
+  };
+  const int b0 = start / ps, b1 = (start + count - 1) / ps;
+  int i0, cnt, off;
+  span(b0, i0, cnt, off);
+  look_up(0);
+  fetch(i0, cnt, now, now_s);
+  for (int b = b0; b <= b1; ++b) {
+    int ni0 = 0, ncnt = 0, noff = 0;
+    if (b < b1) {
+      span(b + 1, ni0, ncnt, noff);
+      if (ni0 + ncnt > tile0 + kCompactTile) { __syncthreads(); look_up(ni0); }
+      fetch(ni0, ncnt, next, next_s);
+    }
+    const int page = table[b];
+    const float old = off > 0 ? scale[(size_t)page * P.Hkv] : 0.0f;
+    float most = old;
+#pragma unroll
+    for (int j = 0; j < MAXV; ++j) most = fmaxf(most, now_s[j]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float* red = s_red[b & 1];
+    if (lane == 0) red[warp] = most;
+    __syncthreads();                            // (all of this block's sources have been read)
+    most = red[lane & 7];
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    uint8_t* to = codes + (size_t)page * page_codes;
+    if (off > 0 && old != most) {
+      const float ratio = old / most;
+      for (int i = tid; i < off * vec_tok; i += kCompactThreads) {
+        uint4 w = *reinterpret_cast<uint4*>(to + ((size_t)i << 4));
+        w.x = e4m3x4_rescale(w.x, ratio); w.y = e4m3x4_rescale(w.y, ratio);
+        w.z = e4m3x4_rescale(w.z, ratio); w.w = e4m3x4_rescale(w.w, ratio);
+        *reinterpret_cast<uint4*>(to + ((size_t)i << 4)) = w;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < MAXV; ++j) {
+      const int x = tid + j * kCompactThreads;
+      if (x < cnt * vec_tok) {
+        uint4 w = now[j];
+        if (now_s[j] != most) {
+          const float ratio = now_s[j] / most;
+          w.x = e4m3x4_rescale(w.x, ratio); w.y = e4m3x4_rescale(w.y, ratio);
+          w.z = e4m3x4_rescale(w.z, ratio); w.w = e4m3x4_rescale(w.w, ratio);
+        }
+        *reinterpret_cast<uint4*>(to + (size_t)off * hd + ((size_t)x << 4)) = w;
+      }
+    }
+    if (tid == 0) scale[(size_t)page * P.Hkv] = most;
+    i0 = ni0; cnt = ncnt; off = noff;
+#pragma unroll
+    for (int j = 0; j < MAXV; ++j) { now[j] = next[j]; now_s[j] = next_s[j]; }
+  }
+}
+
+}  // namespace tabed

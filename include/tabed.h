@@ -360,7 +360,7 @@ int tabed_static_last_error(int32_t device, void* stream);
  *   TABED_ERR_NUMERIC       tabed_pages_append met a value that is not finite (NaN is stored as 0, infinities as +-448 scale)
  *   TABED_ERR_TIMEOUT       a bounded wait ran out */
 typedef struct {
-  void *k, *v;                 /* e4m3 codes [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], 16-byte aligned */
+  void *k, *v;                 /* e4m3 codes [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], 32-byte aligned */
   float *k_scale, *v_scale;    /* [n_layers][n_pages][n_kv_heads], > 0 */
   int32_t *table;              /* [n_seqs][max_pages]: the page of every block of page_tokens tokens, -1 = none */
   int32_t *ref;                /* [n_pages]: entries of `table` that name the page; 0 = free */

@@ -50,13 +50,6 @@ struct TcGemmArgs {
   int* err;
 };
 
-__device__ __forceinline__ uint64_t tc_smem_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  // shared-memory matrix descriptor: start address, leading (K) and stride (row group) byte offsets in
-  // 16-byte units, descriptor version 1 (bits 46-47), no swizzle (bits 61-63 = 0)
-  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16) |
-         ((uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46);
-}
-
 __device__ __forceinline__ bool tc_wait(uint64_t* bar, unsigned parity, int* err) {
   unsigned spins = 0;
   while (!mbar_try_wait(bar, parity)) {

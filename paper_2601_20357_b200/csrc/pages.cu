@@ -9,6 +9,7 @@
 
 #include "../../include/tabed.h"
 #include "pages_attn.cuh"
+#include "pages_attn_tc.cuh"
 #include "pages_kernels.cuh"
 
 using namespace tabed;
@@ -37,7 +38,7 @@ int check(const tabed_pages* p) {
       (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) || p->device < 0 || p->device >= kMaxDevices ||
       (long long)p->max_pages * p->page_tokens > 0x7FFFFF00ll || (long long)p->n_seqs * p->max_pages > 0x7FFFFFFFll || p->n_kv_heads > 1024 || p->n_layers > 32767)
     return TABED_ERR_INVALID_ARG;
-  if (!aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->workspace, 16)) return TABED_ERR_INVALID_ARG;
+  if (!aligned(p->k, 32) || !aligned(p->v, 32) || !aligned(p->workspace, 16)) return TABED_ERR_INVALID_ARG;
   return TABED_OK;
 }
 
@@ -58,9 +59,10 @@ size_t fork_bytes(const tabed_pages* p) {
   return round16((size_t)p->n_seqs * sizeof(ForkEntry)) + 16 + round16((size_t)p->n_seqs * p->max_pages * 4) + round16(fork_free_pages(p) * 4);
 }
 // the attention's: partial results of the segments at both ends of a CTA's part, their maxima and sums, what they belong to
-size_t attn_part_bytes(const tabed_pages* p) { return (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * p->head_dim * 4; }
+constexpr size_t kPartRows = 2 * (size_t)std::max(kPgaMaxCtas * kPgaMaxRows, kPtMaxCtas * kPtMaxRows);
+size_t attn_part_bytes(const tabed_pages* p) { return kPartRows * p->head_dim * 4; }
 size_t attn_bytes(const tabed_pages* p) {
-  return attn_part_bytes(p) + (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * 2 * 4 + (size_t)kPgaMaxCtas * 2 * sizeof(int4);
+  return attn_part_bytes(p) + kPartRows * 2 * 4 + (size_t)kPgaMaxCtas * 2 * sizeof(int4);
 }
 
 // As a programmatic dependent of the kernel before it in the stream: every kernel here waits before it touches memory.
@@ -107,20 +109,34 @@ int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
   static int per_sm[kMaxDevices] = {0};
   if (per_sm[p->device] == 0) {
     int n = 0;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pga_smem<HD>()) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kPgaThreads, pga_smem<HD>()) != cudaSuccess || n < 1) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pga_smem<HD, R8>()) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kPgaThreads, pga_smem<HD, R8>()) != cudaSuccess || n < 1) {
       cudaGetLastError();
       return TABED_ERR_CUDA;
     }
     per_sm[p->device] = n;
   }
   const int ctas = std::min(kPgaMaxCtas, per_sm[p->device] * sm_count(p->device));
-  const int rc = launch(p, kern, dim3(ctas), kPgaThreads, pga_smem<HD>(), a);
+  const int rc = launch(p, kern, dim3(ctas), kPgaThreads, pga_smem<HD, R8>(), a);
   return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas), 256, 0, a);
+}
+
+template <int HD, int MT>
+int launch_attn_tc(const tabed_pages* p, const PagesAttnArgs& a) {
+  auto kern = k_pages_attn_tc<HD, MT>;
+  static bool set[kMaxDevices] = {false};
+  if (!set[p->device]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPtSmem) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+    set[p->device] = true;
+  }
+  const int ctas = std::min(kPtMaxCtas, sm_count(p->device));
+  const int rc = launch(p, kern, dim3(ctas), Pt<HD, MT>::kThreads, kPtSmem, a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, false>, dim3(ctas), 256, 0, a);
 }
 
 template <int HD>
 int launch_attn_hd(const tabed_pages* p, const PagesAttnArgs& a, bool f32) {
+  if (a.part_rows == kPtMaxRows) return a.RB > 128 ? launch_attn_tc<HD, 2>(p, a) : launch_attn_tc<HD, 1>(p, a);
   if (a.RB == 8) return f32 ? launch_attn<HD, true, true>(p, a) : launch_attn<HD, false, true>(p, a);
   return f32 ? launch_attn<HD, true, false>(p, a) : launch_attn<HD, false, false>(p, a);
 }
@@ -233,12 +249,15 @@ int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {
   const long long rows = (long long)t->max_new * (t->n_heads / p->n_kv_heads);
   a.WR = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
   a.RB = rows <= 8 ? 8 : 16 * a.WR;
-  // (an entry's chunks are counted in 31 bits, its rows too)
-  const long long tiles = ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) + a.RB - 1) / a.RB, chunks = ((long long)p->max_pages * p->page_tokens + 63) / 64;
-  if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFFF0ll || tiles * p->n_kv_heads > 0x7FFFFFFFll / chunks) return TABED_ERR_UNSUPPORTED;
+  if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFFF0ll) return TABED_ERR_UNSUPPORTED;      // (an entry's rows are counted in 31 bits)
+  a.part_rows = kPgaMaxRows;
+  if (t->dtype == TABED_DTYPE_BF16 && rows > 16) {
+    a.RB = rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 ? 128 : 256));
+    a.part_rows = kPtMaxRows;
+  }
   unsigned char* ws = static_cast<unsigned char*>(p->workspace);
   a.part = reinterpret_cast<float*>(ws); ws += attn_part_bytes(p);
-  a.part_ml = reinterpret_cast<float*>(ws); ws += (size_t)kPgaMaxCtas * 2 * kPgaMaxRows * 2 * 4;
+  a.part_ml = reinterpret_cast<float*>(ws); ws += kPartRows * 2 * 4;
   a.desc = reinterpret_cast<int4*>(ws);
   OnDevice guard(p->device);
   if (!guard.ok) return TABED_ERR_CUDA;

@@ -25,12 +25,14 @@ namespace tabed {
 
 constexpr int kPgaWarps = 4;                     // consumers
 constexpr int kPgaThreads = 32 * (kPgaWarps + 1);
-constexpr int kPgaMaxCtas = 512;
+constexpr int kPgaMaxCtas = 512;                 // of kPgaMaxRows query rows each, or kPtMaxCtas of kPtMaxRows (pages_attn_tc.cuh)
 constexpr int kPgaMaxRows = 16 * kPgaWarps;      // query rows of a CTA
 template <int HD> __host__ __device__ constexpr int pga_chunk() { return HD == 128 ? 64 : 128; }
 template <int HD> __host__ __device__ constexpr int pga_stages() { return 4; }
 template <int HD> __host__ __device__ constexpr int pga_stage_bytes() { return 2 * pga_chunk<HD>() * HD; }
-template <int HD> __host__ __device__ constexpr size_t pga_smem() { return (size_t)pga_stages<HD>() * pga_stage_bytes<HD>() + (size_t)kPgaMaxRows * (HD + 2) * 4; }
+// stages, and the states of the warps at a segment's end: 64 rows (4 slices of 16, 2 of 32, 1 of 64), or 4 slices of 8
+template <int HD, bool R8> __host__ __device__ constexpr int pga_state_rows() { return R8 ? 8 * kPgaWarps : kPgaMaxRows; }
+template <int HD, bool R8> __host__ __device__ constexpr size_t pga_smem() { return (size_t)pga_stages<HD>() * pga_stage_bytes<HD>() + (size_t)pga_state_rows<HD, R8>() * (HD + 2) * 4; }
 
 struct PagesAttnArgs {
   PagesDev P;
@@ -43,12 +45,13 @@ struct PagesAttnArgs {
   const float* slopes;
   const int* prefix;
   const unsigned long long* tree;
-  float* part;                        // [kPgaMaxCtas][2][rows][hd] partial outputs, then [..][rows][2] maxima and sums
+  float* part;                        // [CTAs][2][part_rows][hd] partial outputs, then [..][rows][2] maxima and sums
   float* part_ml;
-  int4* desc;                         // [kPgaMaxCtas][2] {valid | finished << 1, entry, KV head, tile of rows}
+  int part_rows;                      // rows of a part
+  int4* desc;                         // [CTAs][2] {valid | finished << 1, entry, KV head, tile of rows}
 };
 
-struct PgaEntry { int seq, q0, nq, len, bad; };
+struct PgaEntry { int seq, q0, nq, len, pre, bad; };
 
 // What an entry asks for, with its lengths brought into range; CTA 0 records `bad`.
 __device__ __forceinline__ PgaEntry pga_entry(const PagesAttnArgs& A, int e) {
@@ -56,15 +59,101 @@ __device__ __forceinline__ PgaEntry pga_entry(const PagesAttnArgs& A, int e) {
   const int f0 = A.first[e], f1 = A.first[e + 1];
   E.seq = A.seq ? A.seq[e] : e;
   E.len = A.length[e];
+  E.pre = A.prefix ? A.prefix[e] : 0;
   E.bad = 0;
-  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens) { E.q0 = 0; E.nq = 0; E.bad = PGERR_INVALID; return E; }
+  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens) { E.q0 = 0; E.nq = 0; E.len = 0; E.pre = 0; E.bad = PGERR_INVALID; return E; }
   E.q0 = f0; E.nq = f1 - f0;
   if (E.seq < 0 || E.seq >= A.P.n_seqs || E.len < 0 || E.nq > A.max_new || (A.tree && E.nq > 64)) { E.seq = 0; E.len = 0; E.bad = PGERR_INVALID; }
   if ((long long)E.len > (long long)A.P.max_pages * A.P.ps) { E.len = 0; E.bad = PERR_KV; }
+  E.pre = min(max(E.pre, 0), E.len);
   return E;
 }
+// positions below this one are seen by query row r of an entry (with a tree: and those of its mask)
+__device__ __forceinline__ int pga_limit(const PagesAttnArgs& A, const PgaEntry& E, int r, int grp) {
+  const int base = E.len - E.nq;
+  return max(0, max(A.tree ? base : min(E.len, base + r / grp + 1), E.pre));
+}
 
-struct PgaWalk { int e, kvh, rt, ch, nrt, nch; };      // entry, KV head, tile of rows, chunk; tiles, chunks of the entry
+// The list of all chunks of CH positions: (entry, KV head, tile of RB query rows, chunk); a tile has the chunks up to the last position that one of
+// its rows sees (one at least, which writes the zeros of rows that see nothing).
+template <int CH>
+struct PgaWalk {
+  int e, kvh, rt, ch, nrt, nch, last;
+  PgaEntry E;
+  __device__ __forceinline__ void tile(const PagesAttnArgs& A, int grp) {
+    last = A.tree ? E.len : pga_limit(A, E, min(E.nq * grp, (rt + 1) * A.RB) - 1, grp);
+    nch = max(1, (last + CH - 1) / CH);
+  }
+  __device__ __forceinline__ void entry(const PagesAttnArgs& A, int grp) {
+    E = pga_entry(A, e);
+    nrt = (int)(((long long)E.nq * grp + A.RB - 1) / A.RB);
+  }
+  __device__ __forceinline__ long long head_chunks(const PagesAttnArgs& A, int grp) {      // of one KV head of the entry
+    long long n = 0;
+    for (rt = 0; rt < nrt; ++rt) { tile(A, grp); n += nch; }
+    return n;
+  }
+  __device__ __forceinline__ void step(const PagesAttnArgs& A, int grp) {                   // to the next chunk; there is one
+    if (++ch < nch) return;
+    ch = 0;
+    if (++rt >= nrt) {
+      rt = 0;
+      if (++kvh >= A.P.Hkv) {
+        kvh = 0;
+        do { ++e; entry(A, grp); } while (nrt == 0 && e + 1 < A.n);
+      }
+    }
+    tile(A, grp);
+  }
+};
+
+struct PgaShare { long long part[16], off; int e, total; };
+
+// The CTA's part of the list (equal lengths over the CTAs that get one): where it begins, and its chunks (0: none).  All THREADS
+// threads take part, each summing a strip of entries.
+template <int CH, int THREADS>
+__device__ __forceinline__ int pga_begin(const PagesAttnArgs& A, PgaShare& S, PgaWalk<CH>& w) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, grp = A.H / A.P.Hkv;
+  const int per = (A.n + THREADS - 1) / THREADS, e0 = min(A.n, tid * per), e1 = min(A.n, e0 + per);
+  long long mine = 0;
+  for (w.e = e0; w.e < e1; ++w.e) {
+    w.entry(A, grp);
+    if (w.E.bad && cta == 0) atomicOr(A.P.err, w.E.bad);
+    mine += w.head_chunks(A, grp) * A.P.Hkv;
+  }
+  long long x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+  if (lane == 31) S.part[warp] = x;
+  if (tid == 0) { S.e = 0; S.off = 0; }
+  __syncthreads();
+  long long before = x - mine, all = 0;
+  for (int i = 0; i < THREADS / 32; ++i) { if (i < warp) before += S.part[i]; all += S.part[i]; }
+  const long long nc = all < gridDim.x ? all : gridDim.x;
+  const long long lo = cta < nc ? all * cta / nc : 0, hi = cta < nc ? all * (cta + 1) / nc : 0;
+  if (lo < hi && before <= lo && lo < before + mine) {
+    long long at = before;
+    for (w.e = e0;; ++w.e) {
+      w.entry(A, grp);
+      const long long c = w.head_chunks(A, grp) * A.P.Hkv;
+      if (lo < at + c) break;
+      at += c;
+    }
+    S.e = w.e; S.off = lo - at;
+  }
+  __syncthreads();
+  if (lo < hi) {
+    w.e = S.e;
+    w.entry(A, grp);
+    const long long per_head = w.head_chunks(A, grp);
+    long long rem = S.off;
+    w.kvh = (int)(rem / per_head);
+    rem -= w.kvh * per_head;
+    for (w.rt = 0;; ++w.rt) { w.tile(A, grp); if (rem < w.nch) break; rem -= w.nch; }
+    w.ch = (int)rem;
+  }
+  return (int)(hi - lo);
+}
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -118,78 +207,26 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   extern __shared__ __align__(128) unsigned char pga_smem_raw[];
   unsigned char* ring = pga_smem_raw;
   float* so = reinterpret_cast<float*>(pga_smem_raw + NS * STAGE);        // [slices][rows][HD] states of the warps at a segment's end
-  float* sml = so + kPgaMaxRows * HD;                                      // [slices][rows][2]
+  float* sml = so + pga_state_rows<HD, R8>() * HD;                                      // [slices][rows][2]
   __shared__ uint64_t full[NS], empty[NS];
   __shared__ float4 meta[NS][CH / 16];           // of 16 positions: scale of k, log2 of v's scale, 1 / it
-  __shared__ long long s_part[kPgaThreads / 32], s_lo, s_hi;
-  __shared__ int s_e;
-  __shared__ long long s_off;
+  __shared__ PgaShare s_share;
   __shared__ int s_dead;
   const PagesDev& P = A.P;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
   const int H = A.H, Hkv = P.Hkv, grp = H / Hkv, ps = P.ps, WR = A.WR, WT = kPgaWarps / WR, RB = R8 ? 8 : 16 * WR;
   if (tid == 0) {
     for (int i = 0; i < NS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kPgaWarps); }
-    s_dead = 0; s_e = A.n;
+    s_dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_trigger();
   pdl_wait();
   if (tid < 2) A.desc[cta * 2 + tid] = make_int4(0, 0, 0, 0);
-  // chunks of an entry
-  auto shape = [&](const PgaEntry& E, PgaWalk& w) { w.nrt = (E.nq * grp + RB - 1) / RB; w.nch = max(1, (E.len + CH - 1) / CH); };
-  auto chunks_of = [&](int e) -> long long {
-    const PgaEntry E = pga_entry(A, e);
-    if (E.bad && cta == 0) atomicOr(P.err, E.bad);
-    PgaWalk w;
-    shape(E, w);
-    return (long long)Hkv * w.nrt * w.nch;
-  };
-  // the CTA's part of the list: every thread sums a strip of entries
-  const int per = (A.n + kPgaThreads - 1) / kPgaThreads, e0 = min(A.n, tid * per), e1 = min(A.n, e0 + per);
-  long long mine = 0, before;
-  for (int e = e0; e < e1; ++e) mine += chunks_of(e);
-  {
-    long long x = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(FULL, x, o); if (lane >= o) x += y; }
-    if (lane == 31) s_part[warp] = x;
-    __syncthreads();
-    before = x - mine;
-    long long all = 0;
-    for (int w = 0; w < kPgaThreads / 32; ++w) { if (w < warp) before += s_part[w]; all += s_part[w]; }
-    const long long nc = all < gridDim.x ? all : gridDim.x;
-    const long long lo = cta < nc ? all * cta / nc : 0, hi = cta < nc ? all * (cta + 1) / nc : 0;
-    if (tid == 0) { s_lo = lo; s_hi = hi; }
-    if (lo < hi && before <= lo && lo < before + mine) {
-      long long at = before;
-      int e = e0;
-      for (;; ++e) { const long long c = chunks_of(e); if (lo < at + c) break; at += c; }
-      s_e = e; s_off = lo - at;
-    }
-  }
-  __syncthreads();
-  const int total = (int)(s_hi - s_lo);
+  PgaWalk<CH> w;
+  const int total = pga_begin<CH, kPgaThreads>(A, s_share, w);
   if (total == 0) return;
-  PgaWalk w;
-  PgaEntry E;
-  auto seek = [&]() {
-    w.e = s_e;
-    E = pga_entry(A, w.e);
-    shape(E, w);
-    const int off = (int)s_off, item = off / w.nch;            // (an entry has fewer than 2^31 chunks: its positions and rows are 31 bits, checked by the host)
-    w.ch = off - item * w.nch; w.kvh = item / w.nrt; w.rt = item - w.kvh * w.nrt;
-  };
-  auto step = [&]() {                            // to the next chunk of the list
-    if (++w.ch < w.nch) return;
-    w.ch = 0;
-    if (++w.rt < w.nrt) return;
-    w.rt = 0;
-    if (++w.kvh < Hkv) return;
-    w.kvh = 0;
-    do { ++w.e; E = pga_entry(A, w.e); shape(E, w); } while (w.nrt == 0 && w.e + 1 < A.n);
-  };
-  seek();
+  PgaEntry& E = w.E;
 
   if (warp == kPgaWarps) {
     // ---- producer ----
@@ -243,7 +280,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
         bulk_g2s(sk + lane * bytes, P.k + at, bytes, &full[st]);
         bulk_g2s(sk + CH * HD + lane * bytes, P.v + at, bytes, &full[st]);
       }
-      if (c + 1 < total) step();
+      if (c + 1 < total) w.step(A, grp);
     }
     if (lane == 0) {                             // the last copies land before the shared memory goes, whatever the consumers did
       for (int i = max(0, c - NS); i < c; ++i) {
@@ -270,20 +307,17 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   auto load_q = [&]() {
     nr = E.nq * grp;
     base = E.len - E.nq;
-    const int pre = A.prefix ? min(max(A.prefix[w.e], 0), E.len) : 0;
     const int r_lo = w.rt * RB + wr * 16, r_hi = min(nr, r_lo + 16) - 1;
     live = r_lo < nr;
-    // positions below `lim` are seen by a row (with a tree: and those of its mask)
-    auto limit = [&](int r) { return A.tree ? max(base, pre) : min(E.len, max(base + r / grp + 1, pre)); };
-    lim_min = live ? max(0, limit(r_lo)) : 0;
-    lim_max = !live ? 0 : (A.tree ? E.len : max(0, limit(r_hi)));
+    lim_min = live ? pga_limit(A, E, r_lo, grp) : 0;
+    lim_max = !live ? 0 : (A.tree ? E.len : pga_limit(A, E, r_hi, grp));
 #pragma unroll
     for (int x = 0; x < (R8 ? 1 : 2); ++x) {
       const int r = r_lo + g + 8 * x;
       const bool there = r < nr;
       const int i = there ? r / grp : 0, h = w.kvh * grp + (there ? r - i * grp : 0);
       pos[x] = base + i;
-      lim[x] = there ? limit(r) : 0;
+      lim[x] = there ? pga_limit(A, E, r, grp) : 0;
       bits[x] = there && A.tree ? A.tree[E.q0 + i] : 0ull;
       slope[x] = there && A.slopes ? A.slopes[h] * log2e : 0.0f;
       float v[HD / 4];
@@ -518,8 +552,8 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
         const bool none = sum == 0.0f;
         put(w.rt * RB + r, d, none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : (sum > 0.0f ? make_float4(v.x * f, v.y * f, v.z * f, v.w * f) : make_float4(sum, sum, sum, sum)));
       } else {
-        *reinterpret_cast<float4*>(A.part + ((size_t)slot * kPgaMaxRows + r) * HD + d) = v;
-        if (d == 0) *reinterpret_cast<float2*>(A.part_ml + ((size_t)slot * kPgaMaxRows + r) * 2) = make_float2(m, sum);
+        *reinterpret_cast<float4*>(A.part + ((size_t)slot * A.part_rows + r) * HD + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(A.part_ml + ((size_t)slot * A.part_rows + r) * 2) = make_float2(m, sum);
       }
     }
     if (!whole && tid == 0) A.desc[slot] = make_int4(1 | (to_end ? 2 : 0), w.e, w.kvh, w.rt);
@@ -541,7 +575,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
     __syncwarp();
     if (lane == 0) mbar_arrive(&empty[st]);
     if (w.ch == w.nch - 1 || c == total - 1) { finish(whole_from, w.ch == w.nch - 1); fresh = true; }
-    if (c + 1 < total) step();
+    if (c + 1 < total) w.step(A, grp);
   }
 }
 
@@ -563,7 +597,7 @@ __global__ void __launch_bounds__(256) k_pages_attn_join(const PagesAttnArgs A) 
   const int n = s_n, e = d.y, kvh = d.z, rt = d.w;
   const PgaEntry E = pga_entry(A, e);
   const int rows = min(RB, E.nq * grp - rt * RB);
-  auto slot = [&](int k) { return (size_t)(k == 0 ? c * 2 + 1 : (c + k) * 2) * kPgaMaxRows; };
+  auto slot = [&](int k) { return (size_t)(k == 0 ? c * 2 + 1 : (c + k) * 2) * A.part_rows; };
   for (int x = tid; x < rows * (HD / 4); x += blockDim.x) {
     const int r = x / (HD / 4), dd = (x - r * (HD / 4)) * 4;
     float m = kPgaFloor, sum = 0.0f;

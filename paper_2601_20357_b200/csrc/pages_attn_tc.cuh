@@ -1,0 +1,564 @@
+// Attention over a paged 8-bit cache on the fifth-generation tensor cores, for more than 16 bf16 query rows a KV head: token trees, verified
+// blocks, chunks of prompts.  The same list of chunks (here of 128 positions), numbers and partial results as pages_attn.cuh.
+//
+//   S [128 rows][128 positions] = Q K^T        Q, K in shared memory (kind::f16, fp32 sums in tensor memory)
+//   O [128 rows][hd]           += P V          P in tensor memory (over its S), V in shared memory
+//
+// * A softmax thread has one row: its maximum, sum and limits are its own, and a position's scales are the same for 16 columns.
+//   MT = 2 tiles of 128 rows share the converted K and V, and one's softmax runs under the other's products; with MT = 1 the scores of the
+//   next chunk are computed meanwhile.  Items of up to 64 (32) rows have them 2 (4) times in the tile, and a copy takes a half (a
+//   quarter) of a chunk's positions: the products cost the same, the softmax a half, and the copies are put together at the end.
+// * Four warps load codes straight into registers, a chunk ahead (a thread has one position; through a ring in shared memory the codes would
+//   cost its bandwidth twice more, which binds), turn them into fp16 and store K and V alike as [dims / 8][128 positions][8 dims]: that is
+//   K's K-major layout and V's MN-major one.  Half of the codes go through the conversion unit (16 a clock and SM, which the
+//   exponentials need too), half are shifted into place, which leaves them 2^8 too small: undone in q and in the output.
+// * One warp walks the list, looks pages and scales up and tells the others; one issues the products.
+// q is scaled by a power of two per row: bf16 values are exact in fp16 down to 2^-21 of their row's largest.  Weights have 11 bits.
+#pragma once
+#include "pages_attn.cuh"
+
+namespace tabed {
+
+constexpr int kPtChunk = 128;
+constexpr int kPtInfo = 8;                     // chunks that are known ahead
+constexpr int kPtMaxCtas = 160, kPtMaxRows = 256;
+constexpr size_t kPtSmem = 216u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
+
+struct PtTile {
+  int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, pad;
+  int page[8];                                 // of 16 positions each; -1: none
+  float4 meta[8];                              // scale of k, log2 of v's scale, 1 / it
+};
+
+template <int HD, int MT> struct Pt {
+  static constexpr int kWarps = 4 * MT + 6, kThreads = 32 * kWarps;
+  static constexpr int kOp = kPtChunk * HD * 2;                        // fp16 operand of 128 rows or positions
+  static constexpr int kQOff = 0, kKOff = MT * kOp, kVOff = kKOff + kOp, kEnd = kVOff + 2 * kOp;
+  static_assert(1024 + kEnd <= (int)kPtSmem, "shared memory");
+};
+
+__device__ __forceinline__ void pt_ld16(uint32_t taddr, float* v) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+                 "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]) : "r"(taddr));
+}
+__device__ __forceinline__ void pt_st16(uint32_t taddr, const uint32_t* u) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
+                 "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]) : "memory");
+}
+__device__ __forceinline__ void pt_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pt_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pt_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void pt_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void pt_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void pt_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void pt_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void pt_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void pt_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pt_elect() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(r));
+  return r != 0;
+}
+// two fp32 operations at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)), "l"(*reinterpret_cast<uint64_t*>(&c)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&d);
+}
+// the four codes of a word as fp16, 2^-8 of their values: sign to bit 15, the rest to bits 7 - 13 (subnormals too).
+// (The codes that are no numbers come out as 480.)  In order: (0, 1), (2, 3).
+__device__ __forceinline__ void e4m3x4_shifted(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t a = __byte_perm(w, 0, 0x1404), b = __byte_perm(w, 0, 0x3424);      // codes in the upper bytes of the halves
+  lo = ((a >> 1) & 0x3F803F80u) | (a & 0x80008000u);
+  hi = ((b >> 1) & 0x3F803F80u) | (b & 0x80008000u);
+}
+struct Row32 { uint32_t w[8]; };
+__device__ __forceinline__ Row32 ldg32(const uint8_t* p) {                          // 32 bytes, 32-byte aligned
+  Row32 r;
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p));
+  return r;
+}
+
+template <int HD, int MT>
+__global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const PagesAttnArgs A) {
+  using L = Pt<HD, MT>;
+  constexpr unsigned FULL = 0xffffffffu;
+  constexpr int W_CONV = 4 * MT, W_LOOK = W_CONV + 4, W_MMA = W_CONV + 5, B_CONV = 1 + MT;       // warps; barriers 1 .. MT are the softmax groups'
+  extern __shared__ __align__(128) unsigned char pt_raw[];
+  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pt_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full, k_empty, v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
+  __shared__ PtTile info[kPtInfo];
+  __shared__ PgaShare s_share;
+  __shared__ float s_cr[128 * MT];               // 1 / scale of the query rows
+  __shared__ float2 s_ml[128];                   // copies of a row put together at an item's end
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_dead;
+  const PagesDev& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0), cta = blockIdx.x;      // (the warp's number as a uniform value)
+  const int Hkv = P.Hkv, grp = A.H / Hkv, ps = P.ps, RB = A.RB;
+  const int RP = MT == 2 ? 128 : (RB < 128 ? RB : 128);      // rows of a tile before they repeat: 128, 64 or 32
+  if (tid == 0) {
+    for (int i = 0; i < kPtInfo; ++i) { mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 4 * MT + 1); }       // (read by the softmax warps and the products')
+    mbar_init(&k_full, 4); mbar_init(&k_empty, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_done[i], 1); }
+    s_dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pt_fence_before();
+  __syncthreads();
+  pt_fence_after();
+  pdl_trigger();                                  // (behind the allocation, as in the other kernels with tensor memory)
+  const uint32_t tmem = s_tmem, tm_o = tmem + 256;      // S: two of 128 columns (of two tiles, or of two chunks), O: one or two
+  pdl_wait();
+  if (tid < 2) A.desc[cta * 2 + tid] = make_int4(0, 0, 0, 0);
+  PgaWalk<kPtChunk> w;
+  const int total = pga_begin<kPtChunk, L::kThreads>(A, s_share, w);
+  volatile int* dead = &s_dead;
+  const float log2e = 1.4426950408889634f;
+  const bool cap = A.softcap > 0.0f;
+
+  if (warp == W_LOOK && total > 0) {
+    // ---- the list ----
+    int cb = -1, ce = -1, ck = -1, pg = -1;       // block that lane 0 has looked up, entry, KV head
+    float pks = 1.0f, pvs = 1.0f;
+    bool fresh = true, from_start = false, ok = true;
+#pragma unroll 1
+    for (int c = 0; c < total; ++c) {
+      const PgaEntry& E = w.E;
+      const int p0 = w.ch * kPtChunk, blk0 = p0 / ps, nblk = (E.len + ps - 1) / ps;
+      if (w.e != ce || blk0 < cb || blk0 + kPtChunk / ps > cb + 32) {
+        cb = blk0; ce = w.e; ck = -1;
+        const int b = cb + lane;
+        pg = b < nblk ? P.table[(size_t)E.seq * P.max_pages + b] : -1;
+        if (b < nblk && (pg < 0 || pg >= P.NP)) { atomicOr(P.err, PGERR_INVALID); pg = -1; }
+      }
+      if (w.kvh != ck) {
+        ck = w.kvh;
+        if (pg >= 0) {
+          const size_t at = ((size_t)A.layer * P.NP + pg) * Hkv + w.kvh;
+          pks = P.k_scale[at]; pvs = P.v_scale[at];
+        }
+      }
+      const int src = ((p0 + lane * 16) / ps - cb) & 31;
+      const float ks = __shfl_sync(FULL, pks, src), vs = __shfl_sync(FULL, pvs, src);
+      const int gp = __shfl_sync(FULL, pg, src);
+      PtTile& T = info[c % kPtInfo];
+      if (c >= kPtInfo) { ok = pga_wait(&i_empty[c % kPtInfo], (unsigned)(c / kPtInfo - 1) & 1u, dead, P.err); ok = __all_sync(FULL, ok); if (!ok) break; }
+      if (lane < 8) {
+        const float lv = fmaxf(lg2_approx(vs), -126.0f);
+        T.page[lane] = gp;
+        T.meta[lane] = gp >= 0 ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+      }
+      if (fresh) from_start = w.ch == 0;
+      if (lane == 0) {
+        T.first = fresh; T.to_end = w.ch == w.nch - 1; T.ends = T.to_end || c == total - 1;
+        T.whole = from_start && T.to_end; T.slot = from_start;
+        T.j0 = p0; T.lim_min = pga_limit(A, E, w.rt * RB, grp); T.lim_max = w.last;
+        T.q0 = E.q0; T.nq = E.nq; T.len = E.len; T.pre = E.pre; T.rt = w.rt; T.kvh = w.kvh; T.e = w.e;
+      }
+      fresh = w.ch == w.nch - 1;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&i_full[c % kPtInfo]);
+      if (c + 1 < total) w.step(A, grp);
+    }
+  } else if (warp == W_MMA && total > 0) {
+    // ---- products (the whole warp walks the loop, so that descriptors and flags stay in uniform registers; one elected lane issues) ----
+    const uint32_t id_s = (1u << 4) | (16u << 17) | (8u << 24);                                      // f16 x f16, both K-major, 128 x 128
+    const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | (8u << 24);           // B MN-major, 128 x hd
+    // a step of 16 in the summed index is a constant on the descriptor's address field (16-byte units)
+    const uint64_t d_q = tc_smem_desc(smem_u32(sm + L::kQOff), 2048, 128), d_k = tc_smem_desc(smem_u32(sm + L::kKOff), 2048, 128);
+    const uint64_t d_v = tc_smem_desc(smem_u32(sm + L::kVOff), 128, 2048);
+    const bool one = pt_elect();
+    bool ok = true;
+    auto scores = [&](int j, int m) {             // S of chunk j for tile m, into buffer b
+      const uint32_t d = tmem + (MT == 2 ? m : (j & 1)) * 128;
+      const uint64_t dq = d_q + (uint64_t)(m * (L::kOp >> 4));
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) pt_mma_ss(d, dq + k * 256, d_k + k * 256, id_s, k > 0);
+        if (m == MT - 1) pt_commit(&k_empty);
+        pt_commit(&s_full[MT == 2 ? m : (j & 1)]);
+      }
+      __syncwarp();
+    };
+    auto output = [&](int j, int m, uint32_t fresh) {      // O of tile m, chunk j
+      const int b = MT == 2 ? m : (j & 1);
+      const uint32_t d = tm_o + m * 128, a = tmem + b * 128;
+      const uint64_t dv = d_v + (uint64_t)((j & 1) * (L::kOp >> 4));
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < kPtChunk / 16; ++k) pt_mma_ts(d, a + k * 8, dv + k * 16, id_o, k > 0 || !fresh);
+        if (m == MT - 1) pt_commit(&v_empty[j & 1]);
+        pt_commit(&o_done[m]);
+      }
+      __syncwarp();
+    };
+    auto wait = [&](uint64_t* bar, unsigned parity) { if (ok) { ok = pga_wait(bar, parity, dead, P.err); ok = __all_sync(FULL, ok); } };
+    auto k_ready = [&](int j) { wait(&k_full, (unsigned)j & 1u); pt_fence_after(); };
+    const int ahead = MT == 2 ? 1 : 2;            // chunks whose scores are asked for before the first output
+    for (int j = 0; j < ahead && j < total && ok; ++j) {
+      k_ready(j);
+      for (int m = 0; m < MT && ok; ++m) scores(j, m);
+    }
+#pragma unroll 1
+    for (int j = 0; j < total && ok; ++j) {
+      wait(&i_full[j % kPtInfo], (unsigned)(j / kPtInfo) & 1u);
+      const uint32_t fresh = __shfl_sync(FULL, info[j % kPtInfo].first, 0);
+      if (lane == 0) mbar_arrive(&i_empty[j % kPtInfo]);
+      const bool more = j + ahead < total;
+#pragma unroll 1
+      for (int m = 0; m < MT && ok; ++m) {
+        if (m == 0) wait(&v_full[j & 1], (unsigned)(j >> 1) & 1u);
+        if (MT == 2) wait(&p_full[m], (unsigned)j & 1u);
+        else wait(&p_full[j & 1], (unsigned)(j >> 1) & 1u);
+        if (!ok) break;
+        pt_fence_after();
+        output(j, m, fresh);
+        if (more) {
+          if (m == 0) k_ready(j + ahead);
+          if (ok) scores(j + ahead, m);
+        }
+      }
+    }
+    // (the products read shared memory and write tensor memory until then)
+    for (int m = 0; m < MT; ++m) wait(&o_done[m], (unsigned)(total - 1) & 1u);
+    if (!ok) __nanosleep(100000);
+  } else if (warp >= W_CONV && warp < W_LOOK) {
+    // ---- conversion ----
+    const int ct = tid - 32 * W_CONV;
+    constexpr int NP = HD / 32;                   // 32-byte pieces of a row of codes
+    const bool vec = A.vec_q;
+    Row32 kr[NP], vr[NP];
+    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NP], bool live) {
+      const int page = T.page[ct >> 4];
+      if (live && page >= 0) {
+        const int in = (T.j0 + ct) % ps;
+        const uint8_t* p = codes + ((((size_t)A.layer * P.NP + page) * Hkv + T.kvh) * ps + in) * HD;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) r[i] = ldg32(p + i * 32);
+      } else {                                    // nobody sees it: zeros (0 * NaN is not 0)
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+          for (int x = 0; x < 8; ++x) r[i].w[x] = 0;
+      }
+    };
+    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        uint4 a, b, c, d;
+        e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
+        e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
+        e4m3x4_shifted(r[i].w[4], c.x, c.y); e4m3x4_shifted(r[i].w[5], c.z, c.w);
+        e4m3x4_shifted(r[i].w[6], d.x, d.y); e4m3x4_shifted(r[i].w[7], d.z, d.w);
+        unsigned char* o = dst + i * 4 * 2048 + ct * 16;
+        *reinterpret_cast<uint4*>(o) = a;
+        *reinterpret_cast<uint4*>(o + 2048) = b;
+        *reinterpret_cast<uint4*>(o + 4096) = c;
+        *reinterpret_cast<uint4*>(o + 6144) = d;
+      }
+    };
+    auto known = [&](int j) { pga_wait(&i_full[j % kPtInfo], (unsigned)(j / kPtInfo) & 1u, dead, P.err); __syncwarp(); };
+    auto done = [&](uint64_t* bar) { pt_fence_async(); __syncwarp(); if (lane == 0) mbar_arrive(bar); };
+    if (total > 0) {
+      known(0);
+      fetch(P.k, info[0], kr, info[0].j0 + ct < info[0].lim_max);
+      fetch(P.v, info[0], vr, info[0].j0 + ct < info[0].lim_max);
+    }
+#pragma unroll 1
+    for (int j = 0; j < total; ++j) {
+      const PtTile& T = info[j % kPtInfo];
+      const PtTile& N = info[(j + 1) % kPtInfo];
+      if (j > 0) { pga_wait(&k_empty, (unsigned)(j - 1) & 1u, dead, P.err); __syncwarp(); }
+      if (T.first) {                              // the item's query rows (all scores of the item before are done): a thread has a row of each tile
+        const int nr = T.nq * grp;
+#pragma unroll 1
+        for (int m = 0; m < MT; ++m) {
+          const int row = T.rt * RB + m * 128 + ct % RP;
+          const bool there = m * 128 + ct % RP < RB && row < nr;
+          const int tok = there ? row / grp : 0, h = T.kvh * grp + (there ? row - tok * grp : 0);
+          const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(A.q) + (long long)(T.q0 + tok) * A.q_stride + (long long)h * HD;
+          float amax = 0.0f;
+          if (there)
+#pragma unroll 1
+            for (int d = 0; d < HD; d += 8) {
+              float f[8];
+              load8(p + d, vec, f);
+#pragma unroll
+              for (int x = 0; x < 8; ++x) amax = fmaxf(amax, fabsf(f[x]));
+            }
+          // the largest value to 2^14 .. 2^15
+          const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
+          const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+          s_cr[m * 128 + ct] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
+          unsigned char* dst = sm + L::kQOff + m * L::kOp + ct * 16;
+#pragma unroll 1
+          for (int d = 0; d < HD; d += 8) {
+            float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (there) load8(p + d, vec, f);
+            const float u = d & 16 ? up : up * (1.0f / 256.0f);       // (dims whose codes are shifted: 2^8 more)
+            *reinterpret_cast<uint4*>(dst + (d >> 3) * 2048) =
+                make_uint4(pack_f16(f[0] * u, f[1] * u), pack_f16(f[2] * u, f[3] * u), pack_f16(f[4] * u, f[5] * u), pack_f16(f[6] * u, f[7] * u));
+          }
+        }
+      }
+      put(sm + L::kKOff, kr);
+      done(&k_full);
+      if (j + 1 < total) { known(j + 1); fetch(P.k, N, kr, N.j0 + ct < N.lim_max); }
+      if (j > 1) { pga_wait(&v_empty[j & 1], (unsigned)((j >> 1) - 1) & 1u, dead, P.err); __syncwarp(); }
+      put(sm + L::kVOff + (j & 1) * L::kOp, vr);
+      done(&v_full[j & 1]);
+      if (j + 1 < total) fetch(P.v, N, vr, N.j0 + ct < N.lim_max);
+    }
+  } else if (warp < W_CONV) {
+    // ---- softmax ----
+    const int m = warp >> 2, row = tid & 127, bar = 1 + m;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_o = tm_o + m * 128 + lanes;
+    const int copies = 128 / RP, part = row / RP, cols = 128 / copies, col0 = part * cols;      // the positions of a chunk that this copy of the row takes
+    float M = kPgaFloor, l = 0.0f, cr = 0.0f, slope = 0.0f;
+    int lim = 0, pos = 0;
+    unsigned long long bits = 0;
+#pragma unroll 1
+    for (int j = 0; j < total; ++j) {
+      const PtTile& T = info[j % kPtInfo];
+      const int b = MT == 2 ? m : (j & 1);
+      const uint32_t t_s = tmem + b * 128 + lanes;
+      pga_wait(&i_full[j % kPtInfo], (unsigned)(j / kPtInfo) & 1u, dead, P.err);
+      pga_wait(&s_full[b], (unsigned)(MT == 2 ? j : (j >> 1)) & 1u, dead, P.err);
+      __syncwarp();
+      pt_fence_after();
+      const int base = T.len - T.nq;
+      if (T.first) {
+        const int rr = T.rt * RB + m * 128 + row % RP;
+        const bool there = m * 128 + row % RP < RB && rr < T.nq * grp;
+        const int i = there ? rr / grp : 0, h = T.kvh * grp + (there ? rr - i * grp : 0);
+        M = kPgaFloor; l = 0.0f;
+        cr = s_cr[m * 128 + row] * (cap ? A.scale / A.softcap : A.scale * log2e);
+        pos = base + i;
+        lim = there ? max(0, max(A.tree ? base : min(T.len, base + i + 1), T.pre)) : 0;
+        slope = there && A.slopes ? A.slopes[h] * log2e : 0.0f;
+        bits = there && A.tree ? A.tree[T.q0 + i] : 0ull;
+      }
+      const bool edge = T.j0 + kPtChunk > T.lim_min, special = cap || A.slopes;
+      // x: exponents of 16 columns (one page's) without the maximum
+      auto exponents = [&](int c, float (&x)[16]) {
+        const float4 mt = T.meta[c >> 4];
+        const float a = cr * mt.x;
+        if (!special) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float2 v = fma2(make_float2(x[i], x[i + 1]), make_float2(a, a), make_float2(mt.y, mt.y));
+            x[i] = v.x; x[i + 1] = v.y;
+          }
+        } else {
+          if (cap) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { x[i] *= a; top = fmaxf(top, fabsf(x[i])); }
+            const float c2 = A.softcap * log2e;
+            if (!__any_sync(FULL, !(top <= 0.5f))) {      // tanh y = y (1 - y^2 / 3 + ...): the next term is 9e-8
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                const float2 y = make_float2(x[i], x[i + 1]), z = mul2(y, y);
+                float2 s = make_float2(0.0035921280f, 0.0035921280f);
+                s = fma2(s, z, make_float2(-0.0088632355f, -0.0088632355f));
+                s = fma2(s, z, make_float2(0.0218694885f, 0.0218694885f));
+                s = fma2(s, z, make_float2(-0.0539682540f, -0.0539682540f));
+                s = fma2(s, z, make_float2(0.1333333333f, 0.1333333333f));
+                s = fma2(s, z, make_float2(-0.3333333333f, -0.3333333333f));
+                s = mul2(fma2(mul2(s, z), y, y), make_float2(c2, c2));
+                x[i] = s.x; x[i + 1] = s.y;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = c2 * (1.0f - 2.0f * rcp_approx(1.0f + ex2_approx(x[i] * (2.0f * log2e))));
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= a;
+          }
+          const float d0 = (float)(pos - T.j0 - c);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = fmaf(-slope, fabsf(d0 - (float)i), x[i]) + mt.y;
+        }
+        if (edge || mt.y == -INFINITY) {
+          const int n = mt.y == -INFINITY ? 0 : lim - T.j0 - c, d = T.j0 + c - base;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            bool seen = i < n;
+            if (A.tree && mt.y != -INFINITY) seen = seen || (d + i >= 0 && d + i < 64 && d + i < T.nq && ((bits >> ((d + i) & 63)) & 1ull));
+            if (!seen) x[i] = -INFINITY;
+          }
+        }
+      };
+      // the largest exponent, then the weights (a second pass over the scores: 128 of them would not stay in registers)
+      float top = -INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < cols; c += 32) {
+        float x[32];
+        pt_ld16(t_s + col0 + c, x);
+        pt_ld16(t_s + col0 + c + 16, x + 16);
+        pt_wait_ld();
+        exponents(col0 + c, *reinterpret_cast<float (*)[16]>(x));
+        exponents(col0 + c + 16, *reinterpret_cast<float (*)[16]>(x + 16));
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) top = fmaxf(top, fmaxf(x[i], x[i + 1]));
+        if (special) {                            // (kept: they cost more than their way)
+          pt_st16(t_s + col0 + c, reinterpret_cast<const uint32_t*>(x));
+          pt_st16(t_s + col0 + c + 16, reinterpret_cast<const uint32_t*>(x) + 16);
+        }
+      }
+      if (special) pt_wait_st();
+      const bool grow = top > M + kPgaSlack;
+      if (__any_sync(FULL, grow)) {
+        const float now = grow ? top : M, f = ex2_approx(M - now);
+        M = now; l *= f;
+        if (!T.first) {
+          pga_wait(&o_done[m], (unsigned)(j - 1) & 1u, dead, P.err);
+          __syncwarp();
+          pt_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 16) {
+            float o[16];
+            pt_ld16(t_o + c, o);
+            pt_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] *= f;
+            pt_st16(t_o + c, reinterpret_cast<const uint32_t*>(o));
+          }
+          pt_wait_st();
+        }
+      }
+      const float Mo = M - kPgaLift;
+#pragma unroll 1
+      for (int c = 0; c < 128; c += 32) {         // the weights take the first half of their scores' columns; the other copies' positions are zeros
+        uint32_t pk[16];
+        // (weights of 32 positions take 16 columns, so none lands on scores that are still to be read)
+        if (copies == 1 || (c >= col0 && c < col0 + cols)) {
+          float x[32];
+          pt_ld16(t_s + c, x);
+          pt_ld16(t_s + c + 16, x + 16);
+          pt_wait_ld();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float4 mt = T.meta[(c >> 4) + h];
+            if (!special) exponents(c + 16 * h, *reinterpret_cast<float (*)[16]>(x + 16 * h));
+            float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
+#pragma unroll
+            for (int i = 16 * h; i < 16 * h + 16; i += 4) {
+              float2 y0 = add2(make_float2(x[i], x[i + 1]), make_float2(-Mo, -Mo)), y1 = add2(make_float2(x[i + 2], x[i + 3]), make_float2(-Mo, -Mo));
+              y0.x = ex2_approx(y0.x); y0.y = ex2_approx(y0.y); y1.x = ex2_approx(y1.x); y1.y = ex2_approx(y1.y);
+              s0 = add2(s0, y0); s1 = add2(s1, y1);
+              pk[i / 2] = pack_f16(y0.x, y0.y);
+              pk[i / 2 + 1] = pack_f16(y1.x, y1.y);
+            }
+            s0 = add2(s0, s1);
+            l = fmaf(s0.x + s0.y, mt.z, l);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = 0;
+        }
+        pt_st16(t_s + (c >> 1), pk);
+      }
+      pt_wait_st();
+      pt_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[b]);
+      if (T.ends) {
+        // the rows of O: the result, or this CTA's part of it
+        pga_wait(&o_done[m], (unsigned)j & 1u, dead, P.err);
+        __syncwarp();
+        pt_fence_after();
+        const int rows = min(RB, T.nq * grp - T.rt * RB), r = m * 128 + row % RP;
+        float sum = l, top2 = M, f = 1.0f;
+        if (copies > 1) {
+          s_ml[row] = make_float2(M, l);
+          pt_sync(bar);
+          sum = 0.0f;
+          for (int k = 0; k < copies; ++k) top2 = fmaxf(top2, s_ml[k * RP + row % RP].x);
+          for (int k = 0; k < copies; ++k) { const float2 y = s_ml[k * RP + row % RP]; sum += y.y * ex2_approx(y.x - top2); }
+          f = ex2_approx(M - top2);
+        }
+        const bool whole = T.whole, mine = r < rows && part == 0 && m * 128 + row % RP < RB;
+        const int rr = T.rt * RB + r, tok = rr / grp, h = T.kvh * grp + rr - tok * grp;
+        const size_t slot = (size_t)(cta * 2 + T.slot) * A.part_rows + r;
+        const float norm = whole ? (sum == 0.0f ? 0.0f : f / sum) : f;
+        const bool nan = whole && !(sum >= 0.0f);
+        float* buf = reinterpret_cast<float*>(sm + L::kEnd);      // [128][17] a block of 16 dims of all copies
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 16) {
+          float o[16];
+          pt_ld16(t_o + c, o);
+          pt_wait_ld();
+          const float g = c & 16 ? norm * 256.0f : norm;          // (the shifted dims)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] = nan ? sum : o[i] * g;
+          if (copies > 1) {
+            if (part > 0)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) buf[row * 17 + i] = o[i];
+            pt_sync(bar);
+            if (part == 0)
+              for (int k = 1; k < copies; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] += buf[(k * RP + row) * 17 + i];
+            pt_sync(bar);
+          }
+          if (mine) {
+            if (whole) {
+              if (sum == 0.0f)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = 0.0f;
+              __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + (long long)(T.q0 + tok) * A.out_stride + (long long)h * HD + c;
+              store8(out, A.vec_q, *reinterpret_cast<float (*)[8]>(o));
+              store8(out + 8, A.vec_q, *reinterpret_cast<float (*)[8]>(o + 8));
+            } else {
+              float4* d = reinterpret_cast<float4*>(A.part + slot * HD + c);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+          }
+        }
+        if (mine && !whole) *reinterpret_cast<float2*>(A.part_ml + slot * 2) = make_float2(top2, sum);
+        if (tid == 0 && !whole) A.desc[cta * 2 + T.slot] = make_int4(1 | (T.to_end ? 2 : 0), T.e, T.kvh, T.rt);
+        pt_fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&i_empty[j % kPtInfo]);
+    }
+  }
+  __syncwarp();
+  pt_fence_before();
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+}  // namespace tabed

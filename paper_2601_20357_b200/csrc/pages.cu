@@ -46,7 +46,7 @@ PagesDev on_device(const tabed_pages* p) {
   PagesDev d;
   d.k = static_cast<uint8_t*>(p->k); d.v = static_cast<uint8_t*>(p->v);
   d.k_scale = p->k_scale; d.v_scale = p->v_scale; d.table = p->table; d.ref = p->ref; d.err = p->err;
-  d.L = p->n_layers; d.NP = p->n_pages; d.Hkv = p->n_kv_heads; d.ps = p->page_tokens; d.hd = p->head_dim;
+  d.L = p->n_layers; d.NP = p->n_pages; d.Hkv = p->n_kv_heads; d.ps = p->page_tokens; d.ls = p->page_tokens == 16 ? 4 : (p->page_tokens == 32 ? 5 : (p->page_tokens == 64 ? 6 : 7)); d.hd = p->head_dim;
   d.n_seqs = p->n_seqs; d.max_pages = p->max_pages;
   return d;
 }
@@ -121,9 +121,9 @@ int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
   return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas), 256, 0, a);
 }
 
-template <int HD, int MT>
+template <int HD, int MT, int COPIES>
 int launch_attn_tc(const tabed_pages* p, const PagesAttnArgs& a) {
-  auto kern = k_pages_attn_tc<HD, MT>;
+  auto kern = k_pages_attn_tc<HD, MT, COPIES>;
   static bool set[kMaxDevices] = {false};
   if (!set[p->device]) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPtSmem) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
@@ -136,7 +136,8 @@ int launch_attn_tc(const tabed_pages* p, const PagesAttnArgs& a) {
 
 template <int HD>
 int launch_attn_hd(const tabed_pages* p, const PagesAttnArgs& a, bool f32) {
-  if (a.part_rows == kPtMaxRows) return a.RB > 128 ? launch_attn_tc<HD, 2>(p, a) : launch_attn_tc<HD, 1>(p, a);
+  if (a.part_rows == kPtMaxRows)
+    return a.RB > 128 ? launch_attn_tc<HD, 2, 1>(p, a) : (a.RB == 128 ? launch_attn_tc<HD, 1, 1>(p, a) : (a.RB == 64 ? launch_attn_tc<HD, 1, 2>(p, a) : launch_attn_tc<HD, 1, 4>(p, a)));
   if (a.RB == 8) return f32 ? launch_attn<HD, true, true>(p, a) : launch_attn<HD, false, true>(p, a);
   return f32 ? launch_attn<HD, true, false>(p, a) : launch_attn<HD, false, false>(p, a);
 }

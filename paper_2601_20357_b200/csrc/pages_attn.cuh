@@ -90,7 +90,10 @@ struct PgaWalk {
   }
   __device__ __forceinline__ long long head_chunks(const PagesAttnArgs& A, int grp) {      // of one KV head of the entry
     long long n = 0;
-    for (rt = 0; rt < nrt; ++rt) { tile(A, grp); n += nch; }
+    rt = 0;
+    if (nrt == 1) { tile(A, grp); return nch; }
+#pragma unroll 1
+    for (; rt < nrt; ++rt) { tile(A, grp); n += nch; }
     return n;
   }
   __device__ __forceinline__ void step(const PagesAttnArgs& A, int grp) {                   // to the next chunk; there is one
@@ -100,6 +103,7 @@ struct PgaWalk {
       rt = 0;
       if (++kvh >= A.P.Hkv) {
         kvh = 0;
+#pragma unroll 1
         do { ++e; entry(A, grp); } while (nrt == 0 && e + 1 < A.n);
       }
     }
@@ -107,15 +111,16 @@ struct PgaWalk {
   }
 };
 
-struct PgaShare { long long part[16], off; int e, total; };
+struct PgaShare { long long part[16]; int e, off; };
 
-// The CTA's part of the list (equal lengths over the CTAs that get one): where it begins, and its chunks (0: none).  All THREADS
-// threads take part, each summing a strip of entries.
+// The CTA's part of the list (lengths over the CTAs differ by one): where it begins, and its chunks (0: none).  All THREADS
+// threads take part, each summing a strip of entries.  (A list of 2^31 chunks, 10^11 positions, is refused.)
 template <int CH, int THREADS>
 __device__ __forceinline__ int pga_begin(const PagesAttnArgs& A, PgaShare& S, PgaWalk<CH>& w) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, grp = A.H / A.P.Hkv;
   const int per = (A.n + THREADS - 1) / THREADS, e0 = min(A.n, tid * per), e1 = min(A.n, e0 + per);
   long long mine = 0;
+#pragma unroll 1
   for (w.e = e0; w.e < e1; ++w.e) {
     w.entry(A, grp);
     if (w.E.bad && cta == 0) atomicOr(A.P.err, w.E.bad);
@@ -127,32 +132,35 @@ __device__ __forceinline__ int pga_begin(const PagesAttnArgs& A, PgaShare& S, Pg
   if (lane == 31) S.part[warp] = x;
   if (tid == 0) { S.e = 0; S.off = 0; }
   __syncthreads();
-  long long before = x - mine, all = 0;
-  for (int i = 0; i < THREADS / 32; ++i) { if (i < warp) before += S.part[i]; all += S.part[i]; }
-  const long long nc = all < gridDim.x ? all : gridDim.x;
-  const long long lo = cta < nc ? all * cta / nc : 0, hi = cta < nc ? all * (cta + 1) / nc : 0;
-  if (lo < hi && before <= lo && lo < before + mine) {
-    long long at = before;
+  long long before = x - mine, all64 = 0;
+#pragma unroll 1
+  for (int i = 0; i < THREADS / 32; ++i) { if (i < warp) before += S.part[i]; all64 += S.part[i]; }
+  if (all64 > 0x7FFFFFFFll) { if (tid == 0) atomicOr(A.P.err, PGERR_INVALID); return 0; }
+  const int all = (int)all64, nc = min(all, (int)gridDim.x), each = nc > 0 ? all / nc : 0, extra = all - each * nc;
+  const int lo = cta * each + min(cta, extra), count = cta < nc ? each + (cta < extra ? 1 : 0) : 0;
+  if (count > 0 && (int)before <= lo && lo < (int)(before + mine)) {
+    int at = (int)before;
+#pragma unroll 1
     for (w.e = e0;; ++w.e) {
       w.entry(A, grp);
-      const long long c = w.head_chunks(A, grp) * A.P.Hkv;
+      const int c = (int)(w.head_chunks(A, grp) * A.P.Hkv);
       if (lo < at + c) break;
       at += c;
     }
     S.e = w.e; S.off = lo - at;
   }
   __syncthreads();
-  if (lo < hi) {
+  if (count > 0) {
     w.e = S.e;
     w.entry(A, grp);
-    const long long per_head = w.head_chunks(A, grp);
-    long long rem = S.off;
-    w.kvh = (int)(rem / per_head);
-    rem -= w.kvh * per_head;
+    const int per_head = (int)w.head_chunks(A, grp);
+    w.kvh = S.off / per_head;
+    int rem = S.off - w.kvh * per_head;
+#pragma unroll 1
     for (w.rt = 0;; ++w.rt) { w.tile(A, grp); if (rem < w.nch) break; rem -= w.nch; }
-    w.ch = (int)rem;
+    w.ch = rem;
   }
-  return (int)(hi - lo);
+  return count;
 }
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -240,7 +248,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
     for (; c < total; ++c) {
       const int st = c % NS;
       if (c >= NS) { ok = pga_wait(&empty[st], (unsigned)(c / NS - 1) & 1u, &s_dead, P.err); ok = __all_sync(FULL, ok); if (!ok) break; }
-      const int p0 = w.ch * CH, blk0 = p0 / ps, nblk = (E.len + ps - 1) / ps;
+      const int p0 = w.ch * CH, blk0 = p0 >> P.ls, nblk = (E.len + ps - 1) >> P.ls;
       if (w.e != ce || blk0 < cb || blk0 + ppc > cb + 32) {
         cb = blk0; ce = w.e; ck = -1;
         const int b = cb + lane;
@@ -259,7 +267,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
       const unsigned bytes = (unsigned)rows * HD, n_has = __popc(__ballot_sync(FULL, has));
       unsigned char* sk = ring + st * STAGE;
       {
-        const int src = ((p0 + lane * 16) / ps - cb) & 31;       // (lanes beyond the chunk's groups read something and drop it)
+        const int src = (((p0 + lane * 16) >> P.ls) - cb) & 31;       // (lanes beyond the chunk's groups read something and drop it)
         const float ks = __shfl_sync(FULL, pks, src), vs = __shfl_sync(FULL, pvs, src);
         const int gp = __shfl_sync(FULL, pg, src);
         if (lane < CH / 16) {
@@ -276,7 +284,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
       if (lane == 0) { if (n_has) mbar_expect_tx(&full[st], 2 * n_has * bytes); else mbar_arrive(&full[st]); }
       __syncwarp();
       if (has) {
-        const size_t at = (((size_t)A.layer * P.NP + mypg) * Hkv + w.kvh) * ps * HD + (size_t)(ps > CH ? p0 % ps : 0) * HD;
+        const size_t at = (((size_t)A.layer * P.NP + mypg) * Hkv + w.kvh) * ps * HD + (size_t)(ps > CH ? p0 & (ps - 1) : 0) * HD;
         bulk_g2s(sk + lane * bytes, P.k + at, bytes, &full[st]);
         bulk_g2s(sk + CH * HD + lane * bytes, P.v + at, bytes, &full[st]);
       }

@@ -25,7 +25,7 @@ constexpr int kPtMaxCtas = 160, kPtMaxRows = 256;
 constexpr size_t kPtSmem = 216u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
 
 struct PtTile {
-  int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, pad;
+  int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, gaps;      // gaps: positions without a page
   int page[8];                                 // of 16 positions each; -1: none
   float4 meta[8];                              // scale of k, log2 of v's scale, 1 / it
 };
@@ -70,6 +70,11 @@ __device__ __forceinline__ bool pt_elect() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(r));
   return r != 0;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // two fp32 operations at a time
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   uint64_t d;
@@ -101,11 +106,11 @@ __device__ __forceinline__ Row32 ldg32(const uint8_t* p) {                      
   return r;
 }
 
-template <int HD, int MT>
+template <int HD, int MT, int COPIES>
 __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const PagesAttnArgs A) {
   using L = Pt<HD, MT>;
   constexpr unsigned FULL = 0xffffffffu;
-  constexpr int W_CONV = 4 * MT, W_LOOK = W_CONV + 4, W_MMA = W_CONV + 5, B_CONV = 1 + MT;       // warps; barriers 1 .. MT are the softmax groups'
+  constexpr int W_CONV = 4 * MT, W_LOOK = W_CONV + 4, W_MMA = W_CONV + 5;       // warps; barriers 1 .. MT are the softmax groups'
   extern __shared__ __align__(128) unsigned char pt_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pt_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full, k_empty, v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
@@ -118,7 +123,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
   const PagesDev& P = A.P;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0), cta = blockIdx.x;      // (the warp's number as a uniform value)
   const int Hkv = P.Hkv, grp = A.H / Hkv, ps = P.ps, RB = A.RB;
-  const int RP = MT == 2 ? 128 : (RB < 128 ? RB : 128);      // rows of a tile before they repeat: 128, 64 or 32
+  constexpr int RP = 128 / COPIES;               // rows of a tile before they repeat
+  constexpr bool ALL = MT == 2;                  // all codes are shifted (the exponentials of 256 rows fill the conversion unit), or half of them
   if (tid == 0) {
     for (int i = 0; i < kPtInfo; ++i) { mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 4 * MT + 1); }       // (read by the softmax warps and the products')
     mbar_init(&k_full, 4); mbar_init(&k_empty, 1);
@@ -152,8 +158,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
 #pragma unroll 1
     for (int c = 0; c < total; ++c) {
       const PgaEntry& E = w.E;
-      const int p0 = w.ch * kPtChunk, blk0 = p0 / ps, nblk = (E.len + ps - 1) / ps;
-      if (w.e != ce || blk0 < cb || blk0 + kPtChunk / ps > cb + 32) {
+      const int p0 = w.ch * kPtChunk, blk0 = p0 >> P.ls, nblk = (E.len + ps - 1) >> P.ls;
+      if (w.e != ce || blk0 < cb || blk0 + (kPtChunk >> P.ls) > cb + 32) {
         cb = blk0; ce = w.e; ck = -1;
         const int b = cb + lane;
         pg = b < nblk ? P.table[(size_t)E.seq * P.max_pages + b] : -1;
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           pks = P.k_scale[at]; pvs = P.v_scale[at];
         }
       }
-      const int src = ((p0 + lane * 16) / ps - cb) & 31;
+      const int src = (((p0 + lane * 16) >> P.ls) - cb) & 31;
       const float ks = __shfl_sync(FULL, pks, src), vs = __shfl_sync(FULL, pvs, src);
       const int gp = __shfl_sync(FULL, pg, src);
       PtTile& T = info[c % kPtInfo];
@@ -177,7 +183,9 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
         T.meta[lane] = gp >= 0 ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
       }
       if (fresh) from_start = w.ch == 0;
+      const bool gaps = __any_sync(FULL, lane < 8 && gp < 0);
       if (lane == 0) {
+        T.gaps = gaps;
         T.first = fresh; T.to_end = w.ch == w.nch - 1; T.ends = T.to_end || c == total - 1;
         T.whole = from_start && T.to_end; T.slot = from_start;
         T.j0 = p0; T.lim_min = pga_limit(A, E, w.rt * RB, grp); T.lim_max = w.last;
@@ -259,7 +267,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NP], bool live) {
       const int page = T.page[ct >> 4];
       if (live && page >= 0) {
-        const int in = (T.j0 + ct) % ps;
+        const int in = (T.j0 + ct) & (ps - 1);
         const uint8_t* p = codes + ((((size_t)A.layer * P.NP + page) * Hkv + T.kvh) * ps + in) * HD;
 #pragma unroll
         for (int i = 0; i < NP; ++i) r[i] = ldg32(p + i * 32);
@@ -270,12 +278,17 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           for (int x = 0; x < 8; ++x) r[i].w[x] = 0;
       }
     };
-    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted
+    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted (or all)
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         uint4 a, b, c, d;
-        e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
-        e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
+        if (ALL) {
+          e4m3x4_shifted(r[i].w[0], a.x, a.y); e4m3x4_shifted(r[i].w[1], a.z, a.w);
+          e4m3x4_shifted(r[i].w[2], b.x, b.y); e4m3x4_shifted(r[i].w[3], b.z, b.w);
+        } else {
+          e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
+          e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
+        }
         e4m3x4_shifted(r[i].w[4], c.x, c.y); e4m3x4_shifted(r[i].w[5], c.z, c.w);
         e4m3x4_shifted(r[i].w[6], d.x, d.y); e4m3x4_shifted(r[i].w[7], d.z, d.w);
         unsigned char* o = dst + i * 4 * 2048 + ct * 16;
@@ -305,27 +318,33 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           const bool there = m * 128 + ct % RP < RB && row < nr;
           const int tok = there ? row / grp : 0, h = T.kvh * grp + (there ? row - tok * grp : 0);
           const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(A.q) + (long long)(T.q0 + tok) * A.q_stride + (long long)h * HD;
-          float amax = 0.0f;
-          if (there)
-#pragma unroll 1
-            for (int d = 0; d < HD; d += 8) {
-              float f[8];
-              load8(p + d, vec, f);
+          uint4 q[HD / 8];                        // (all on their way at once)
+          uint32_t top = 0;
 #pragma unroll
-              for (int x = 0; x < 8; ++x) amax = fmaxf(amax, fabsf(f[x]));
+          for (int d = 0; d < HD / 8; ++d) {
+            q[d] = make_uint4(0, 0, 0, 0);
+            if (there) {
+              if (vec) q[d] = *reinterpret_cast<const uint4*>(p + d * 8);
+              else {
+                const unsigned short* u = reinterpret_cast<const unsigned short*>(p + d * 8);
+                q[d] = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+              }
             }
+          }
+#pragma unroll
+          for (int d = 0; d < HD / 8; ++d)
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(q[d].x & 0x7FFF7FFFu, q[d].y & 0x7FFF7FFFu), __vmaxu2(q[d].z & 0x7FFF7FFFu, q[d].w & 0x7FFF7FFFu)));
+          const float amax = __uint_as_float(max(top & 0xFFFFu, top >> 16) << 16);
           // the largest value to 2^14 .. 2^15
           const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
           const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
           s_cr[m * 128 + ct] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
           unsigned char* dst = sm + L::kQOff + m * L::kOp + ct * 16;
-#pragma unroll 1
-          for (int d = 0; d < HD; d += 8) {
-            float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            if (there) load8(p + d, vec, f);
-            const float u = d & 16 ? up : up * (1.0f / 256.0f);       // (dims whose codes are shifted: 2^8 more)
-            *reinterpret_cast<uint4*>(dst + (d >> 3) * 2048) =
-                make_uint4(pack_f16(f[0] * u, f[1] * u), pack_f16(f[2] * u, f[3] * u), pack_f16(f[4] * u, f[5] * u), pack_f16(f[6] * u, f[7] * u));
+#pragma unroll
+          for (int d = 0; d < HD / 8; ++d) {
+            const float u = ALL || (d & 2) ? up : up * (1.0f / 256.0f);       // (dims whose codes are shifted: 2^8 more)
+            auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * u, __uint_as_float(v & 0xFFFF0000u) * u); };
+            *reinterpret_cast<uint4*>(dst + d * 2048) = make_uint4(half2(q[d].x), half2(q[d].y), half2(q[d].z), half2(q[d].w));
           }
         }
       }
@@ -341,7 +360,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     // ---- softmax ----
     const int m = warp >> 2, row = tid & 127, bar = 1 + m;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_o = tm_o + m * 128 + lanes;
-    const int copies = 128 / RP, part = row / RP, cols = 128 / copies, col0 = part * cols;      // the positions of a chunk that this copy of the row takes
+    constexpr int COLS = 128 / COPIES;            // the positions of a chunk that this copy of the row takes, from col0 on
+    const int part = COPIES == 1 ? 0 : row / RP, col0 = part * COLS;
     float M = kPgaFloor, l = 0.0f, cr = 0.0f, slope = 0.0f;
     int lim = 0, pos = 0;
     unsigned long long bits = 0;
@@ -350,13 +370,12 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       const PtTile& T = info[j % kPtInfo];
       const int b = MT == 2 ? m : (j & 1);
       const uint32_t t_s = tmem + b * 128 + lanes;
-      pga_wait(&i_full[j % kPtInfo], (unsigned)(j / kPtInfo) & 1u, dead, P.err);
       pga_wait(&s_full[b], (unsigned)(MT == 2 ? j : (j >> 1)) & 1u, dead, P.err);
       __syncwarp();
       pt_fence_after();
-      const int base = T.len - T.nq;
-      if (T.first) {
-        const int rr = T.rt * RB + m * 128 + row % RP;
+      const bool first = T.first;
+      if (first) {
+        const int rr = T.rt * RB + m * 128 + row % RP, base = T.len - T.nq;
         const bool there = m * 128 + row % RP < RB && rr < T.nq * grp;
         const int i = there ? rr / grp : 0, h = T.kvh * grp + (there ? rr - i * grp : 0);
         M = kPgaFloor; l = 0.0f;
@@ -366,22 +385,22 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
         slope = there && A.slopes ? A.slopes[h] * log2e : 0.0f;
         bits = there && A.tree ? A.tree[T.q0 + i] : 0ull;
       }
-      const bool edge = T.j0 + kPtChunk > T.lim_min, special = cap || A.slopes;
-      // x: exponents of 16 columns (one page's) without the maximum
-      auto exponents = [&](int c, float (&x)[16]) {
-        const float4 mt = T.meta[c >> 4];
-        const float a = cr * mt.x;
-        if (!special) {
+      // Caps, biases and masks first, in place (16 columns, one page's, at a time); then every chunk is alike.
+      const bool pre = cap || A.slopes || T.j0 + kPtChunk > T.lim_min || T.gaps;
+      if (pre) {
+#pragma unroll 1
+        for (int c = col0; c < col0 + COLS; c += 16) {
+          float x[16];
+          pt_ld16(t_s + c, x);
+          const float4 mt = T.meta[c >> 4];
+          const float a = cr * mt.x;
+          pt_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float2 v = fma2(make_float2(x[i], x[i + 1]), make_float2(a, a), make_float2(mt.y, mt.y));
-            x[i] = v.x; x[i + 1] = v.y;
-          }
-        } else {
+          for (int i = 0; i < 16; ++i) x[i] *= a;
           if (cap) {
             float top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) { x[i] *= a; top = fmaxf(top, fabsf(x[i])); }
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
             const float c2 = A.softcap * log2e;
             if (!__any_sync(FULL, !(top <= 0.5f))) {      // tanh y = y (1 - y^2 / 3 + ...): the next term is 9e-8
 #pragma unroll
@@ -400,47 +419,56 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
 #pragma unroll
               for (int i = 0; i < 16; ++i) x[i] = c2 * (1.0f - 2.0f * rcp_approx(1.0f + ex2_approx(x[i] * (2.0f * log2e))));
             }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= a;
           }
-          const float d0 = (float)(pos - T.j0 - c);
+          if (A.slopes) {
+            const float d0 = (float)(pos - T.j0 - c);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = fmaf(-slope, fabsf(d0 - (float)i), x[i]) + mt.y;
-        }
-        if (edge || mt.y == -INFINITY) {
-          const int n = mt.y == -INFINITY ? 0 : lim - T.j0 - c, d = T.j0 + c - base;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            bool seen = i < n;
-            if (A.tree && mt.y != -INFINITY) seen = seen || (d + i >= 0 && d + i < 64 && d + i < T.nq && ((bits >> ((d + i) & 63)) & 1ull));
-            if (!seen) x[i] = -INFINITY;
+            for (int i = 0; i < 16; ++i) x[i] = fmaf(-slope, fabsf(d0 - (float)i), x[i]);
           }
-        }
-      };
-      // the largest exponent, then the weights (a second pass over the scores: 128 of them would not stay in registers)
-      float top = -INFINITY;
-#pragma unroll 1
-      for (int c = 0; c < cols; c += 32) {
-        float x[32];
-        pt_ld16(t_s + col0 + c, x);
-        pt_ld16(t_s + col0 + c + 16, x + 16);
-        pt_wait_ld();
-        exponents(col0 + c, *reinterpret_cast<float (*)[16]>(x));
-        exponents(col0 + c + 16, *reinterpret_cast<float (*)[16]>(x + 16));
+          if (T.j0 + c + 16 > T.lim_min || mt.y == -INFINITY) {
+            uint32_t seen = 0;                    // of 16 positions
+            if (mt.y != -INFINITY) {
+              const int n = lim - T.j0 - c, d = T.j0 + c - (T.len - T.nq);
+              seen = n >= 16 ? 0xFFFFu : (n > 0 ? (1u << n) - 1u : 0u);
+              if (A.tree && d > -16 && d < 64) {
+                uint32_t t = (uint32_t)(d >= 0 ? bits >> d : bits << -d);
+                const int behind = T.nq - d;      // rows of the entry from here on
+                seen |= t & (behind >= 16 ? 0xFFFFu : (behind > 0 ? (1u << behind) - 1u : 0u));
+              }
+            }
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) top = fmaxf(top, fmaxf(x[i], x[i + 1]));
-        if (special) {                            // (kept: they cost more than their way)
-          pt_st16(t_s + col0 + c, reinterpret_cast<const uint32_t*>(x));
-          pt_st16(t_s + col0 + c + 16, reinterpret_cast<const uint32_t*>(x) + 16);
+            for (int i = 0; i < 16; ++i) if (!((seen >> i) & 1u)) x[i] = -INFINITY;
+          }
+          pt_st16(t_s + c, reinterpret_cast<const uint32_t*>(x));
         }
+        pt_wait_st();
       }
-      if (special) pt_wait_st();
+      // The largest exponent: of 16 raw scores, then scaled (the next ones are on their way meanwhile).
+      float top = -INFINITY;
+      {
+        float x[2][16];
+        pt_ld16(t_s + col0, x[0]);
+#pragma unroll 1
+        for (int c = 0; c < COLS; c += 32) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float4 mt = T.meta[(col0 + c + 16 * h) >> 4];
+            const float a = pre ? 1.0f : cr * mt.x, *y = x[h];
+            pt_wait_ld();
+            pt_ld16(t_s + ((col0 + c + 16 * h + 16) & 127), x[h ^ 1]);
+            float t = max3(y[0], y[1], y[2]);
+#pragma unroll
+            for (int i = 3; i < 15; i += 2) t = max3(t, y[i], y[i + 1]);
+            top = max3(top, fmaf(fmaxf(t, y[15]), a, mt.y), top);
+          }
+        }
+        pt_wait_ld();
+      }
       const bool grow = top > M + kPgaSlack;
       if (__any_sync(FULL, grow)) {
         const float now = grow ? top : M, f = ex2_approx(M - now);
         M = now; l *= f;
-        if (!T.first) {
+        if (!first) {
           pga_wait(&o_done[m], (unsigned)(j - 1) & 1u, dead, P.err);
           __syncwarp();
           pt_fence_after();
@@ -456,37 +484,43 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           pt_wait_st();
         }
       }
-      const float Mo = M - kPgaLift;
+      // The weights: those of 32 positions take 16 columns, behind which the scores have been read; the positions of the other copies are zeros.
+      {
+        const float Mo = M - kPgaLift;
+        float x[2][16];
+        pt_ld16(t_s + col0, x[0]);
 #pragma unroll 1
-      for (int c = 0; c < 128; c += 32) {         // the weights take the first half of their scores' columns; the other copies' positions are zeros
-        uint32_t pk[16];
-        // (weights of 32 positions take 16 columns, so none lands on scores that are still to be read)
-        if (copies == 1 || (c >= col0 && c < col0 + cols)) {
-          float x[32];
-          pt_ld16(t_s + c, x);
-          pt_ld16(t_s + c + 16, x + 16);
-          pt_wait_ld();
+        for (int c = 0; c < COLS; c += 32) {
+          uint32_t pk[16];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float4 mt = T.meta[(c >> 4) + h];
-            if (!special) exponents(c + 16 * h, *reinterpret_cast<float (*)[16]>(x + 16 * h));
+            const float4 mt = T.meta[(col0 + c + 16 * h) >> 4];
+            const float a = pre ? 1.0f : cr * mt.x, bb = mt.y - Mo, *y = x[h];
+            pt_wait_ld();
+            pt_ld16(t_s + ((col0 + c + 16 * h + 16) & 127), x[h ^ 1]);
             float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
 #pragma unroll
-            for (int i = 16 * h; i < 16 * h + 16; i += 4) {
-              float2 y0 = add2(make_float2(x[i], x[i + 1]), make_float2(-Mo, -Mo)), y1 = add2(make_float2(x[i + 2], x[i + 3]), make_float2(-Mo, -Mo));
+            for (int i = 0; i < 16; i += 4) {
+              float2 y0 = fma2(make_float2(y[i], y[i + 1]), make_float2(a, a), make_float2(bb, bb)), y1 = fma2(make_float2(y[i + 2], y[i + 3]), make_float2(a, a), make_float2(bb, bb));
               y0.x = ex2_approx(y0.x); y0.y = ex2_approx(y0.y); y1.x = ex2_approx(y1.x); y1.y = ex2_approx(y1.y);
               s0 = add2(s0, y0); s1 = add2(s1, y1);
-              pk[i / 2] = pack_f16(y0.x, y0.y);
-              pk[i / 2 + 1] = pack_f16(y1.x, y1.y);
+              pk[8 * h + i / 2] = pack_f16(y0.x, y0.y);
+              pk[8 * h + i / 2 + 1] = pack_f16(y1.x, y1.y);
             }
             s0 = add2(s0, s1);
             l = fmaf(s0.x + s0.y, mt.z, l);
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) pk[i] = 0;
+          pt_st16(t_s + ((col0 + c) >> 1), pk);
         }
-        pt_st16(t_s + (c >> 1), pk);
+        pt_wait_ld();
+        if (COPIES > 1) {
+          uint32_t none[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) none[i] = 0;
+#pragma unroll 1
+          for (int c = 0; c < 64; c += 16)
+            if (c < (col0 >> 1) || c >= (col0 + COLS) >> 1) pt_st16(t_s + c, none);
+        }
       }
       pt_wait_st();
       pt_fence_before();
@@ -499,12 +533,12 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
         pt_fence_after();
         const int rows = min(RB, T.nq * grp - T.rt * RB), r = m * 128 + row % RP;
         float sum = l, top2 = M, f = 1.0f;
-        if (copies > 1) {
+        if (COPIES > 1) {
           s_ml[row] = make_float2(M, l);
           pt_sync(bar);
           sum = 0.0f;
-          for (int k = 0; k < copies; ++k) top2 = fmaxf(top2, s_ml[k * RP + row % RP].x);
-          for (int k = 0; k < copies; ++k) { const float2 y = s_ml[k * RP + row % RP]; sum += y.y * ex2_approx(y.x - top2); }
+          for (int k = 0; k < COPIES; ++k) top2 = fmaxf(top2, s_ml[k * RP + row % RP].x);
+          for (int k = 0; k < COPIES; ++k) { const float2 y = s_ml[k * RP + row % RP]; sum += y.y * ex2_approx(y.x - top2); }
           f = ex2_approx(M - top2);
         }
         const bool whole = T.whole, mine = r < rows && part == 0 && m * 128 + row % RP < RB;
@@ -518,16 +552,16 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           float o[16];
           pt_ld16(t_o + c, o);
           pt_wait_ld();
-          const float g = c & 16 ? norm * 256.0f : norm;          // (the shifted dims)
+          const float g = ALL || (c & 16) ? norm * 256.0f : norm;          // (the shifted dims)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] = nan ? sum : o[i] * g;
-          if (copies > 1) {
+          if (COPIES > 1) {
             if (part > 0)
 #pragma unroll
               for (int i = 0; i < 16; ++i) buf[row * 17 + i] = o[i];
             pt_sync(bar);
             if (part == 0)
-              for (int k = 1; k < copies; ++k)
+              for (int k = 1; k < COPIES; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[i] += buf[(k * RP + row) * 17 + i];
             pt_sync(bar);

@@ -20,7 +20,7 @@ struct PagesDev {
   uint8_t *k, *v;
   float *k_scale, *v_scale;
   int *table, *ref, *err;
-  int L, NP, Hkv, ps, hd, n_seqs, max_pages;
+  int L, NP, Hkv, ps, ls, hd, n_seqs, max_pages;      // ps = 1 << ls tokens a page
 };
 
 // ---- e4m3 ------------------------------------------------------------------------------------------

@@ -365,7 +365,7 @@ typedef struct {
   int32_t *table;              /* [n_seqs][max_pages]: the page of every block of page_tokens tokens, -1 = none */
   int32_t *ref;                /* [n_pages]: entries of `table` that name the page; 0 = free */
   int32_t *err;                /* [1] */
-  void *workspace;             /* tabed_pages_workspace bytes, 16-byte aligned; contents need not be kept between calls */
+  void *workspace;             /* tabed_pages_workspace bytes, 32-byte aligned; contents need not be kept between calls */
   int32_t n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_seqs, max_pages;
                                /* page_tokens 16, 32, 64 or 128; head_dim 32, 64 or 128; n_seqs <= 32767 */
   int32_t device;

@@ -38,7 +38,7 @@ int check(const tabed_pages* p) {
       (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) || p->device < 0 || p->device >= kMaxDevices ||
       (long long)p->max_pages * p->page_tokens > 0x7FFFFF00ll || (long long)p->n_seqs * p->max_pages > 0x7FFFFFFFll || p->n_kv_heads > 1024 || p->n_layers > 32767)
     return TABED_ERR_INVALID_ARG;
-  if (!aligned(p->k, 32) || !aligned(p->v, 32) || !aligned(p->workspace, 16)) return TABED_ERR_INVALID_ARG;
+  if (!aligned(p->k, 32) || !aligned(p->v, 32) || !aligned(p->workspace, 32)) return TABED_ERR_INVALID_ARG;
   return TABED_OK;
 }
 
@@ -118,7 +118,7 @@ int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
   }
   const int ctas = std::min(kPgaMaxCtas, per_sm[p->device] * sm_count(p->device));
   const int rc = launch(p, kern, dim3(ctas), kPgaThreads, pga_smem<HD, R8>(), a);
-  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas), 256, 0, a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas, (a.RB + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, a);
 }
 
 template <int HD, int MT, int COPIES>
@@ -131,13 +131,13 @@ int launch_attn_tc(const tabed_pages* p, const PagesAttnArgs& a) {
   }
   const int ctas = std::min(kPtMaxCtas, sm_count(p->device));
   const int rc = launch(p, kern, dim3(ctas), Pt<HD, MT>::kThreads, kPtSmem, a);
-  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, false>, dim3(ctas), 256, 0, a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, false>, dim3(ctas, (a.RB + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, a);
 }
 
 template <int HD>
 int launch_attn_hd(const tabed_pages* p, const PagesAttnArgs& a, bool f32) {
   if (a.part_rows == kPtMaxRows)
-    return a.RB > 128 ? launch_attn_tc<HD, 2, 1>(p, a) : (a.RB == 128 ? launch_attn_tc<HD, 1, 1>(p, a) : (a.RB == 64 ? launch_attn_tc<HD, 1, 2>(p, a) : launch_attn_tc<HD, 1, 4>(p, a)));
+    return a.RB == 256 ? launch_attn_tc<HD, 2, 1>(p, a) : (a.RB == 128 ? launch_attn_tc<HD, 1, 1>(p, a) : launch_attn_tc<HD, 1, 2>(p, a));
   if (a.RB == 8) return f32 ? launch_attn<HD, true, true>(p, a) : launch_attn<HD, false, true>(p, a);
   return f32 ? launch_attn<HD, true, false>(p, a) : launch_attn<HD, false, false>(p, a);
 }
@@ -253,7 +253,7 @@ int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {
   if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFFF0ll) return TABED_ERR_UNSUPPORTED;      // (an entry's rows are counted in 31 bits)
   a.part_rows = kPgaMaxRows;
   if (t->dtype == TABED_DTYPE_BF16 && rows > 16) {
-    a.RB = rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 ? 128 : 256));
+    a.RB = rows <= 64 ? 64 : (rows <= 128 ? 128 : 256);
     a.part_rows = kPtMaxRows;
   }
   unsigned char* ws = static_cast<unsigned char*>(p->workspace);

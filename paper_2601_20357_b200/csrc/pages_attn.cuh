@@ -16,7 +16,7 @@
 // Numbers.  q is scaled by a power of two per row and rounded to fp16: exact for bf16 values; fp32 rows take a second term (22 bits).
 // With v's scale inside the exponent, w_j = 2^(s_j log2 e + log2 vs_j - M), the sum of w V needs no scale and the sum of
 // weights is that of w_j / vs_j.  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
-// M only moves when a score exceeds it by more than 2^3, so the sums are rarely rescaled.
+// M only moves when a score exceeds it by more than 6, so the sums are rarely rescaled.
 // Sequences that span CTAs are put together by k_pages_attn_join from the partial results, in fixed order.
 #pragma once
 #include "pages_kernels.cuh"
@@ -26,6 +26,7 @@ namespace tabed {
 constexpr int kPgaWarps = 4;                     // consumers
 constexpr int kPgaThreads = 32 * (kPgaWarps + 1);
 constexpr int kPgaMaxCtas = 512;                 // of kPgaMaxRows query rows each, or kPtMaxCtas of kPtMaxRows (pages_attn_tc.cuh)
+constexpr int kPgaStart = 3;                     // chunks that an item's beginning and end cost
 constexpr int kPgaMaxRows = 16 * kPgaWarps;      // query rows of a CTA
 template <int HD> __host__ __device__ constexpr int pga_chunk() { return HD == 128 ? 64 : 128; }
 template <int HD> __host__ __device__ constexpr int pga_stages() { return 4; }
@@ -111,54 +112,75 @@ struct PgaWalk {
   }
 };
 
-struct PgaShare { long long part[16]; int e, off; };
+struct PgaShare { long long part[16][2]; int e, kvh, rt, ch, chunk[2]; };
 
-// The CTA's part of the list (lengths over the CTAs differ by one): where it begins, and its chunks (0: none).  All THREADS
-// threads take part, each summing a strip of entries.  (A list of 2^31 chunks, 10^11 positions, is refused.)
-template <int CH, int THREADS>
+// The CTA's part of the list: where it begins, and its chunks (0: none).  Beginning and ending an item costs about START chunks, so the list
+// is cut into equal parts of chunks and that many more per item: a part of short sequences has fewer chunks.  All THREADS threads take part,
+// each summing a strip of entries.  (A list of 2^31 chunks, 10^11 positions, is refused.)
+template <int CH, int START, int THREADS>
 __device__ __forceinline__ int pga_begin(const PagesAttnArgs& A, PgaShare& S, PgaWalk<CH>& w) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, grp = A.H / A.P.Hkv;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, grp = A.H / A.P.Hkv, Hkv = A.P.Hkv;
   const int per = (A.n + THREADS - 1) / THREADS, e0 = min(A.n, tid * per), e1 = min(A.n, e0 + per);
-  long long mine = 0;
+  long long mine = 0, chunks = 0;                // cost, chunks of the strip
 #pragma unroll 1
   for (w.e = e0; w.e < e1; ++w.e) {
     w.entry(A, grp);
     if (w.E.bad && cta == 0) atomicOr(A.P.err, w.E.bad);
-    mine += w.head_chunks(A, grp) * A.P.Hkv;
+    const long long c = w.head_chunks(A, grp) * Hkv;
+    chunks += c;
+    mine += c + (long long)w.nrt * START * Hkv;
   }
-  long long x = mine;
+  long long x = mine, y = chunks;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-  if (lane == 31) S.part[warp] = x;
-  if (tid == 0) { S.e = 0; S.off = 0; }
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long a = __shfl_up_sync(0xffffffffu, x, o), b = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) { x += a; y += b; }
+  }
+  if (lane == 31) { S.part[warp][0] = x; S.part[warp][1] = y; }
+  if (tid < 2) S.chunk[tid] = 0;
   __syncthreads();
-  long long before = x - mine, all64 = 0;
+  long long before = x - mine, chunks_before = y - chunks, all64 = 0, all_chunks = 0;
 #pragma unroll 1
-  for (int i = 0; i < THREADS / 32; ++i) { if (i < warp) before += S.part[i]; all64 += S.part[i]; }
+  for (int i = 0; i < THREADS / 32; ++i) {
+    if (i < warp) { before += S.part[i][0]; chunks_before += S.part[i][1]; }
+    all64 += S.part[i][0]; all_chunks += S.part[i][1];
+  }
   if (all64 > 0x7FFFFFFFll) { if (tid == 0) atomicOr(A.P.err, PGERR_INVALID); return 0; }
-  const int all = (int)all64, nc = min(all, (int)gridDim.x), each = nc > 0 ? all / nc : 0, extra = all - each * nc;
-  const int lo = cta * each + min(cta, extra), count = cta < nc ? each + (cta < extra ? 1 : 0) : 0;
-  if (count > 0 && (int)before <= lo && lo < (int)(before + mine)) {
-    int at = (int)before;
+  const int all = (int)all64, nc = min((int)all_chunks, (int)gridDim.x), each = nc > 0 ? all / nc : 0, extra = all - each * nc;
+  // both ends of the part in the list
 #pragma unroll 1
-    for (w.e = e0;; ++w.e) {
-      w.entry(A, grp);
-      const int c = (int)(w.head_chunks(A, grp) * A.P.Hkv);
-      if (lo < at + c) break;
-      at += c;
+  for (int end = 0; end < 2; ++end) {
+    const int c = cta + end, at = c >= nc ? all : c * each + min(c, extra);
+    if (at >= all) { if (tid == 0) S.chunk[end] = (int)all_chunks; continue; }
+    if ((int)before <= at && at < (int)(before + mine)) {
+      int left = at - (int)before, done = (int)chunks_before, per_head = 0, cost = 0;
+#pragma unroll 1
+      for (w.e = e0;; ++w.e) {
+        w.entry(A, grp);
+        per_head = (int)w.head_chunks(A, grp);
+        cost = per_head + w.nrt * START;
+        if (left < cost * Hkv) break;
+        left -= cost * Hkv;
+        done += per_head * Hkv;
+      }
+      const int kvh = left / cost;
+      left -= kvh * cost;
+      done += kvh * per_head;
+#pragma unroll 1
+      for (w.rt = 0;; ++w.rt) { w.tile(A, grp); if (left < w.nch + START) break; left -= w.nch + START; done += w.nch; }
+      // (an item's start is not divided: whoever is cut in it has the item's first chunk first)
+      const int ch = max(0, left - START);
+      S.chunk[end] = done + ch;
+      if (end == 0) { S.e = w.e; S.kvh = kvh; S.rt = w.rt; S.ch = ch; }
     }
-    S.e = w.e; S.off = lo - at;
   }
   __syncthreads();
+  const int count = S.chunk[1] - S.chunk[0];
   if (count > 0) {
-    w.e = S.e;
+    w.e = S.e; w.kvh = S.kvh; w.rt = S.rt;
     w.entry(A, grp);
-    const int per_head = (int)w.head_chunks(A, grp);
-    w.kvh = S.off / per_head;
-    int rem = S.off - w.kvh * per_head;
-#pragma unroll 1
-    for (w.rt = 0;; ++w.rt) { w.tile(A, grp); if (rem < w.nch) break; rem -= w.nch; }
-    w.ch = rem;
+    w.tile(A, grp);
+    w.ch = S.ch;
   }
   return count;
 }
@@ -204,7 +226,7 @@ template <> struct PgaBytes<16> {
 };
 
 constexpr float kPgaFloor = -1e30f;              // the running maximum of a row that has seen nothing
-constexpr float kPgaSlack = 3.0f, kPgaLift = 12.0f;      // weights are at most 2^(slack + lift) = 2^15
+constexpr float kPgaSlack = 6.0f, kPgaLift = 9.0f;       // weights are at most 2^(slack + lift) = 2^15
 
 // TWO: fp32 rows (two fp16 terms of q and of the weights).  R8: no entry has more than 8 rows a KV head.
 template <int HD, bool TWO, bool R8>
@@ -232,7 +254,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   pdl_wait();
   if (tid < 2) A.desc[cta * 2 + tid] = make_int4(0, 0, 0, 0);
   PgaWalk<CH> w;
-  const int total = pga_begin<CH, kPgaThreads>(A, s_share, w);
+  const int total = pga_begin<CH, kPgaStart, kPgaThreads>(A, s_share, w);
   if (total == 0) return;
   PgaEntry& E = w.E;
 
@@ -587,51 +609,94 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   }
 }
 
-// Puts the parts of the items that span CTAs together: block c takes the item that begins in CTA c and goes on behind it.
+// Puts the parts of the items that span CTAs together: block (c, y) takes four rows of the item that begins in CTA c and goes on behind
+// it.  The weights of all parts come first (their loads are independent), then the parts' outputs, split over the threads that the rows leave.
+constexpr int kJoinRows = 4, kJoinThreads = 256;
+
 template <int HD, bool TWO>
-__global__ void __launch_bounds__(256) k_pages_attn_join(const PagesAttnArgs A) {
+__global__ void __launch_bounds__(kJoinThreads) k_pages_attn_join(const PagesAttnArgs A) {
+  constexpr int ITEMS = kJoinRows * HD / 4, SPLIT = kJoinThreads / ITEMS, PER_ROW = kJoinThreads / kJoinRows;
+  __shared__ float s_f[kJoinRows][kPgaMaxCtas + 1], s_red[kJoinRows][2][PER_ROW / 32], s_sum[kJoinRows];
+  __shared__ float4 s_v[SPLIT > 1 ? SPLIT - 1 : 1][ITEMS];
   __shared__ int s_n;
-  const int c = blockIdx.x, tid = threadIdx.x, grp = A.H / A.P.Hkv, RB = A.RB;
+  const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, grp = A.H / A.P.Hkv, RB = A.RB, r0 = blockIdx.y * kJoinRows;
   pdl_trigger();
   pdl_wait();
   const int4 d = A.desc[c * 2 + 1];
   if (!(d.x & 1)) return;
-  if (tid == 0) {                                // CTAs that have a part of it
+  const int e = d.y, kvh = d.z, rt = d.w;
+  const PgaEntry E = pga_entry(A, e);
+  const int rows = min(RB, E.nq * grp - rt * RB) - r0;
+  if (rows <= 0) return;
+  if (tid < 32) {                                // CTAs that have a part: up to the first that has its end
     int n = 1;
-    while (c + n < gridDim.x) { const int x = A.desc[(c + n) * 2].x; if (!(x & 1)) break; ++n; if (x & 2) break; }
-    s_n = n;
+    for (int k = 1;; k += 32) {
+      const int x = c + k + lane < (int)gridDim.x ? A.desc[(c + k + lane) * 2].x : 0;
+      const unsigned stop = __ballot_sync(0xffffffffu, !(x & 1) || (x & 2)), ends = __ballot_sync(0xffffffffu, (x & 3) == 3);
+      if (stop) { const int at = __ffs(stop) - 1; n += at + ((ends >> at) & 1); break; }
+      n += 32;
+    }
+    if (lane == 0) s_n = n;
   }
   __syncthreads();
-  const int n = s_n, e = d.y, kvh = d.z, rt = d.w;
-  const PgaEntry E = pga_entry(A, e);
-  const int rows = min(RB, E.nq * grp - rt * RB);
-  auto slot = [&](int k) { return (size_t)(k == 0 ? c * 2 + 1 : (c + k) * 2) * A.part_rows; };
-  for (int x = tid; x < rows * (HD / 4); x += blockDim.x) {
-    const int r = x / (HD / 4), dd = (x - r * (HD / 4)) * 4;
+  const int n = s_n;
+  auto slot = [&](int k) { return (size_t)(k == 0 ? c * 2 + 1 : (c + k) * 2) * A.part_rows + r0; };
+  {
+    const int r = tid / PER_ROW, t = tid - r * PER_ROW, w = t >> 5;
     float m = kPgaFloor, sum = 0.0f;
-    for (int k = 0; k < n; ++k) m = fmaxf(m, A.part_ml[(slot(k) + r) * 2]);
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-      const float2 ml = *reinterpret_cast<const float2*>(A.part_ml + (slot(k) + r) * 2);
+    if (r < rows)
+      for (int k = t; k < n; k += PER_ROW) { const float x = A.part_ml[(slot(k) + r) * 2]; s_f[r][k] = x; m = fmaxf(m, x); }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) s_red[r][0][w] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER_ROW / 32; ++i) m = fmaxf(m, s_red[r][0][i]);
+    if (r < rows)
+      for (int k = t; k < n; k += PER_ROW) {
+        const float f = ex2_approx(s_f[r][k] - m);
+        s_f[r][k] = f;
+        sum += A.part_ml[(slot(k) + r) * 2 + 1] * f;
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_red[r][1][w] = sum;
+    __syncthreads();
+    if (tid < kJoinRows) {
+      float x = 0.0f;
+#pragma unroll
+      for (int i = 0; i < PER_ROW / 32; ++i) x += s_red[tid][1][i];
+      s_sum[tid] = x;
+    }
+    __syncthreads();
+  }
+  const int item = tid % ITEMS, part = tid / ITEMS, r = item / (HD / 4), dd = (item - r * (HD / 4)) * 4;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (r < rows) {
+#pragma unroll 8
+    for (int k = part; k < n; k += SPLIT) {
       const float4 u = *reinterpret_cast<const float4*>(A.part + (slot(k) + r) * HD + dd);
-      const float f = ex2_approx(ml.x - m);
-      sum += ml.y * f;
+      const float f = s_f[r][k];
       v.x += u.x * f; v.y += u.y * f; v.z += u.z * f; v.w += u.w * f;
     }
-    const int row = rt * RB + r, i = row / grp, h = kvh * grp + row - i * grp;
-    const long long at = (long long)(E.q0 + i) * A.out_stride + (long long)h * HD + dd;
-    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
-    v = sum == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : (sum > 0.0f ? make_float4(v.x * f, v.y * f, v.z * f, v.w * f) : make_float4(sum, sum, sum, sum));
-    if (TWO) {
-      float* p = reinterpret_cast<float*>(A.out) + at;
-      if (A.vec_q) *reinterpret_cast<float4*>(p) = v;
-      else { p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w; }
-    } else {
-      __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(A.out) + at;
-      if (A.vec_q) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-      else { p[0] = __float2bfloat16_rn(v.x); p[1] = __float2bfloat16_rn(v.y); p[2] = __float2bfloat16_rn(v.z); p[3] = __float2bfloat16_rn(v.w); }
-    }
+  }
+  if (part > 0) s_v[part - 1][item] = v;
+  __syncthreads();
+  if (part > 0 || r >= rows) return;
+#pragma unroll
+  for (int k = 0; k < SPLIT - 1; ++k) { const float4 u = s_v[k][item]; v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w; }
+  const float sum = s_sum[r], f = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const int row = rt * RB + r0 + r, i = row / grp, h = kvh * grp + row - i * grp;
+  const long long at = (long long)(E.q0 + i) * A.out_stride + (long long)h * HD + dd;
+  v = sum == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : (sum > 0.0f ? make_float4(v.x * f, v.y * f, v.z * f, v.w * f) : make_float4(sum, sum, sum, sum));
+  if (TWO) {
+    float* p = reinterpret_cast<float*>(A.out) + at;
+    if (A.vec_q) *reinterpret_cast<float4*>(p) = v;
+    else { p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w; }
+  } else {
+    __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(A.out) + at;
+    if (A.vec_q) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    else { p[0] = __float2bfloat16_rn(v.x); p[1] = __float2bfloat16_rn(v.y); p[2] = __float2bfloat16_rn(v.z); p[3] = __float2bfloat16_rn(v.w); }
   }
 }
 

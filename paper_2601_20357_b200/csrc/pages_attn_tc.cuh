@@ -4,10 +4,10 @@
 //   S [128 rows][128 positions] = Q K^T        Q, K in shared memory (kind::f16, fp32 sums in tensor memory)
 //   O [128 rows][hd]           += P V          P in tensor memory (over its S), V in shared memory
 //
-// * A softmax thread has one row: its maximum, sum and limits are its own, and a position's scales are the same for 16 columns.
-//   MT = 2 tiles of 128 rows share the converted K and V, and one's softmax runs under the other's products; with MT = 1 the scores of the
-//   next chunk are computed meanwhile.  Items of up to 64 (32) rows have them 2 (4) times in the tile, and a copy takes a half (a
-//   quarter) of a chunk's positions: the products cost the same, the softmax a half, and the copies are put together at the end.
+// * A softmax thread has one row: its limits and its running maximum are scalars, and a position's scales are the same for 16 columns.
+//   MT = 2 tiles of 128 rows share the converted K and V, and one's softmax runs under the other's products; with MT = 1 two threads have a
+//   row, half of a chunk's positions each, and the scores of the next chunk are computed meanwhile.  Items of up to 64 rows have them twice in
+//   the tile, and a copy takes half of the positions: the products cost the same, the softmax a half; the copies are put together at the end.
 // * Four warps load codes straight into registers, a chunk ahead (a thread has one position; through a ring in shared memory the codes would
 //   cost its bandwidth twice more, which binds), turn them into fp16 and store K and V alike as [dims / 8][128 positions][8 dims]: that is
 //   K's K-major layout and V's MN-major one.  Half of the codes go through the conversion unit (16 a clock and SM, which the
@@ -20,9 +20,10 @@
 namespace tabed {
 
 constexpr int kPtChunk = 128;
+constexpr int kPtStart = 2;                    // chunks that an item's beginning and end cost
 constexpr int kPtInfo = 8;                     // chunks that are known ahead
 constexpr int kPtMaxCtas = 160, kPtMaxRows = 256;
-constexpr size_t kPtSmem = 216u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
+constexpr size_t kPtSmem = 162u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
 
 struct PtTile {
   int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, gaps;      // gaps: positions without a page
@@ -31,7 +32,7 @@ struct PtTile {
 };
 
 template <int HD, int MT> struct Pt {
-  static constexpr int kWarps = 4 * MT + 6, kThreads = 32 * kWarps;
+  static constexpr int kThreads = 32 * 14;                             // 8 warps for the softmax, 4, 1, 1
   static constexpr int kOp = kPtChunk * HD * 2;                        // fp16 operand of 128 rows or positions
   static constexpr int kQOff = 0, kKOff = MT * kOp, kVOff = kKOff + kOp, kEnd = kVOff + 2 * kOp;
   static_assert(1024 + kEnd <= (int)kPtSmem, "shared memory");
@@ -64,7 +65,7 @@ __device__ __forceinline__ void pt_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
 __device__ __forceinline__ void pt_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void pt_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void pt_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void pt_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+template <int ID, int N> __device__ __forceinline__ void pt_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
 __device__ __forceinline__ bool pt_elect() {
   uint32_t r;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}\n" : "=r"(r));
@@ -99,36 +100,42 @@ __device__ __forceinline__ void e4m3x4_shifted(uint32_t w, uint32_t& lo, uint32_
   hi = ((b >> 1) & 0x3F803F80u) | (b & 0x80008000u);
 }
 struct Row32 { uint32_t w[8]; };
-__device__ __forceinline__ Row32 ldg32(const uint8_t* p) {                          // 32 bytes, 32-byte aligned
+// 32 bytes, 32-byte aligned, or zeros.  (One predicated load: behind a branch around it the warp would wait for the value.)
+__device__ __forceinline__ Row32 ldg32_if(const uint8_t* p, bool there) {
   Row32 r;
-  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.w[i] = 0;
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %9, 0;\n @p ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n}\n"
+               : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]), "+r"(r.w[4]), "+r"(r.w[5]), "+r"(r.w[6]), "+r"(r.w[7]) : "l"(p), "r"((int)there));
   return r;
+}
+__device__ __forceinline__ void stg32(void* p, const uint32_t* u) {                 // 32 bytes, 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
 }
 
 template <int HD, int MT, int COPIES>
 __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const PagesAttnArgs A) {
   using L = Pt<HD, MT>;
   constexpr unsigned FULL = 0xffffffffu;
-  constexpr int W_CONV = 4 * MT, W_LOOK = W_CONV + 4, W_MMA = W_CONV + 5;       // warps; barriers 1 .. MT are the softmax groups'
+  constexpr int W_CONV = 8, W_LOOK = 12, W_MMA = 13;
   extern __shared__ __align__(128) unsigned char pt_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pt_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full, k_empty, v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
   __shared__ PtTile info[kPtInfo];
   __shared__ PgaShare s_share;
   __shared__ float s_cr[128 * MT];               // 1 / scale of the query rows
-  __shared__ float2 s_ml[128];                   // copies of a row put together at an item's end
+  __shared__ float s_top[2][2][128];             // MT = 1: the largest exponents of both halves of the positions
+  __shared__ float2 s_ml[2][128];                // ... and (maximum, sum) at an item's end
   __shared__ uint32_t s_tmem;
   __shared__ int s_dead;
   const PagesDev& P = A.P;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0), cta = blockIdx.x;      // (the warp's number as a uniform value)
   const int Hkv = P.Hkv, grp = A.H / Hkv, ps = P.ps, RB = A.RB;
   constexpr int RP = 128 / COPIES;               // rows of a tile before they repeat
-  constexpr bool ALL = MT == 2;                  // all codes are shifted (the exponentials of 256 rows fill the conversion unit), or half of them
   if (tid == 0) {
-    for (int i = 0; i < kPtInfo; ++i) { mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 4 * MT + 1); }       // (read by the softmax warps and the products')
+    for (int i = 0; i < kPtInfo; ++i) { mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 9); }       // (read by the softmax warps and the products')
     mbar_init(&k_full, 4); mbar_init(&k_empty, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_done[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], MT == 2 ? 4 : 8); mbar_init(&o_done[i], 1); }
     s_dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -141,11 +148,13 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
   __syncthreads();
   pt_fence_after();
   pdl_trigger();                                  // (behind the allocation, as in the other kernels with tensor memory)
-  const uint32_t tmem = s_tmem, tm_o = tmem + 256;      // S: two of 128 columns (of two tiles, or of two chunks), O: one or two
+  // S: two of 128 columns (of two tiles, or of two chunks); O: one or two.  The weights lie over their scores, whose halves two threads
+  // read with MT = 1: there they have columns of their own.
+  const uint32_t tmem = s_tmem, tm_o = tmem + 256;
   pdl_wait();
   if (tid < 2) A.desc[cta * 2 + tid] = make_int4(0, 0, 0, 0);
   PgaWalk<kPtChunk> w;
-  const int total = pga_begin<kPtChunk, L::kThreads>(A, s_share, w);
+  const int total = pga_begin<kPtChunk, kPtStart, L::kThreads>(A, s_share, w);
   volatile int* dead = &s_dead;
   const float log2e = 1.4426950408889634f;
   const bool cap = A.softcap > 0.0f;
@@ -218,7 +227,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     };
     auto output = [&](int j, int m, uint32_t fresh) {      // O of tile m, chunk j
       const int b = MT == 2 ? m : (j & 1);
-      const uint32_t d = tm_o + m * 128, a = tmem + b * 128;
+      const uint32_t d = tm_o + m * 128, a = MT == 2 ? tmem + b * 128 : tmem + 384 + b * 64;
       const uint64_t dv = d_v + (uint64_t)((j & 1) * (L::kOp >> 4));
       if (one) {
 #pragma unroll
@@ -260,108 +269,107 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     if (!ok) __nanosleep(100000);
   } else if (warp >= W_CONV && warp < W_LOOK) {
     // ---- conversion ----
-    const int ct = tid - 32 * W_CONV;
-    constexpr int NP = HD / 32;                   // 32-byte pieces of a row of codes
+    // A warp has 32 positions.  A lane has one 32-byte piece of every (32 / RS)th of them: eight neighbouring lanes have
+    // neighbouring positions (stores free of bank conflicts), and together the lanes read whole rows (few lines a load).
+    const int ct = tid - 32 * W_CONV, cw = ct >> 5;
+    constexpr int NP = HD / 32, RS = 32 / NP;
+    const int piece = lane / RS, row0 = cw * 32 + lane % RS;
     const bool vec = A.vec_q;
     Row32 kr[NP], vr[NP];
-    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NP], bool live) {
-      const int page = T.page[ct >> 4];
-      if (live && page >= 0) {
-        const int in = (T.j0 + ct) & (ps - 1);
-        const uint8_t* p = codes + ((((size_t)A.layer * P.NP + page) * Hkv + T.kvh) * ps + in) * HD;
+    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NP]) {
+      const uint8_t* base = codes + ((size_t)A.layer * P.NP * Hkv + T.kvh) * (ps * HD) + piece * 32;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) r[i] = ldg32(p + i * 32);
-      } else {                                    // nobody sees it: zeros (0 * NaN is not 0)
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-          for (int x = 0; x < 8; ++x) r[i].w[x] = 0;
+      for (int i = 0; i < NP; ++i) {
+        const int at = row0 + i * RS, page = T.page[at >> 4];
+        const bool there = page >= 0 && T.j0 + at < T.lim_max;      // (what nobody sees becomes zeros: 0 * NaN is not 0)
+        r[i] = ldg32_if(base + (there ? (size_t)page * Hkv * (ps * HD) + (size_t)((T.j0 + at) & (ps - 1)) * HD : 0), there);
       }
     };
-    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted (or all)
+    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted
+      unsigned char* o = dst + piece * 4 * 2048 + row0 * 16;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         uint4 a, b, c, d;
-        if (ALL) {
-          e4m3x4_shifted(r[i].w[0], a.x, a.y); e4m3x4_shifted(r[i].w[1], a.z, a.w);
-          e4m3x4_shifted(r[i].w[2], b.x, b.y); e4m3x4_shifted(r[i].w[3], b.z, b.w);
-        } else {
-          e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
-          e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
-        }
+        e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
+        e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
         e4m3x4_shifted(r[i].w[4], c.x, c.y); e4m3x4_shifted(r[i].w[5], c.z, c.w);
         e4m3x4_shifted(r[i].w[6], d.x, d.y); e4m3x4_shifted(r[i].w[7], d.z, d.w);
-        unsigned char* o = dst + i * 4 * 2048 + ct * 16;
-        *reinterpret_cast<uint4*>(o) = a;
-        *reinterpret_cast<uint4*>(o + 2048) = b;
-        *reinterpret_cast<uint4*>(o + 4096) = c;
-        *reinterpret_cast<uint4*>(o + 6144) = d;
+        *reinterpret_cast<uint4*>(o + i * RS * 16) = a;
+        *reinterpret_cast<uint4*>(o + i * RS * 16 + 2048) = b;
+        *reinterpret_cast<uint4*>(o + i * RS * 16 + 4096) = c;
+        *reinterpret_cast<uint4*>(o + i * RS * 16 + 6144) = d;
       }
     };
     auto known = [&](int j) { pga_wait(&i_full[j % kPtInfo], (unsigned)(j / kPtInfo) & 1u, dead, P.err); __syncwarp(); };
     auto done = [&](uint64_t* bar) { pt_fence_async(); __syncwarp(); if (lane == 0) mbar_arrive(bar); };
     if (total > 0) {
       known(0);
-      fetch(P.k, info[0], kr, info[0].j0 + ct < info[0].lim_max);
-      fetch(P.v, info[0], vr, info[0].j0 + ct < info[0].lim_max);
+      fetch(P.k, info[0], kr);
+      fetch(P.v, info[0], vr);
     }
 #pragma unroll 1
     for (int j = 0; j < total; ++j) {
       const PtTile& T = info[j % kPtInfo];
       const PtTile& N = info[(j + 1) % kPtInfo];
       if (j > 0) { pga_wait(&k_empty, (unsigned)(j - 1) & 1u, dead, P.err); __syncwarp(); }
-      if (T.first) {                              // the item's query rows (all scores of the item before are done): a thread has a row of each tile
-        const int nr = T.nq * grp;
+      if (T.first) {                              // the item's query rows (all scores of the item before are done): a lane has every fourth 16-byte piece
+        const int nr = T.nq * grp;                // of 8 rows a step, so that four lanes read 64 bytes of a row
 #pragma unroll 1
-        for (int m = 0; m < MT; ++m) {
-          const int row = T.rt * RB + m * 128 + ct % RP;
-          const bool there = m * 128 + ct % RP < RB && row < nr;
-          const int tok = there ? row / grp : 0, h = T.kvh * grp + (there ? row - tok * grp : 0);
-          const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(A.q) + (long long)(T.q0 + tok) * A.q_stride + (long long)h * HD;
-          uint4 q[HD / 8];                        // (all on their way at once)
-          uint32_t top = 0;
+        for (int step = 0; step < 4 * MT; ++step) {
+          const int at = (step >> 2) * 128 + cw * 32 + (step & 3) * 8 + (lane & 7), r = (step >> 2) * 128 + (at & 127) % RP, row = T.rt * RB + r;
+          const bool there = r < RB && row < nr;
+          const int tok = there ? row / grp : 0, h = T.kvh * grp + (there ? row - tok * grp : 0), d0 = (lane >> 3) * 8;
+          const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(A.q) + (long long)(T.q0 + tok) * A.q_stride + (long long)h * HD + d0;
+          uint4 q[NP];
 #pragma unroll
-          for (int d = 0; d < HD / 8; ++d) {
-            q[d] = make_uint4(0, 0, 0, 0);
-            if (there) {
-              if (vec) q[d] = *reinterpret_cast<const uint4*>(p + d * 8);
-              else {
-                const unsigned short* u = reinterpret_cast<const unsigned short*>(p + d * 8);
-                q[d] = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
-              }
+          for (int i = 0; i < NP; ++i) q[i] = make_uint4(0, 0, 0, 0);
+          if (there) {
+            if (vec) {
+#pragma unroll
+              for (int i = 0; i < NP; ++i) q[i] = *reinterpret_cast<const uint4*>(p + i * 32);
+            } else {
+              const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+              for (int i = 0; i < NP; ++i)
+                q[i] = make_uint4(u[i * 32] | (uint32_t)u[i * 32 + 1] << 16, u[i * 32 + 2] | (uint32_t)u[i * 32 + 3] << 16,
+                                  u[i * 32 + 4] | (uint32_t)u[i * 32 + 5] << 16, u[i * 32 + 6] | (uint32_t)u[i * 32 + 7] << 16);
             }
           }
+          uint32_t top = 0;
 #pragma unroll
-          for (int d = 0; d < HD / 8; ++d)
-            top = __vmaxu2(top, __vmaxu2(__vmaxu2(q[d].x & 0x7FFF7FFFu, q[d].y & 0x7FFF7FFFu), __vmaxu2(q[d].z & 0x7FFF7FFFu, q[d].w & 0x7FFF7FFFu)));
-          const float amax = __uint_as_float(max(top & 0xFFFFu, top >> 16) << 16);
+          for (int i = 0; i < NP; ++i)
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(q[i].x & 0x7FFF7FFFu, q[i].y & 0x7FFF7FFFu), __vmaxu2(q[i].z & 0x7FFF7FFFu, q[i].w & 0x7FFF7FFFu)));
+          top = max(top & 0xFFFFu, top >> 16);
+          top = max(top, __shfl_xor_sync(FULL, top, 8));
+          top = max(top, __shfl_xor_sync(FULL, top, 16));
           // the largest value to 2^14 .. 2^15
-          const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127, -100), 127);
+          const int ex = min(max((int)(top >> 7) - 127, -100), 127);
           const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-          s_cr[m * 128 + ct] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
-          unsigned char* dst = sm + L::kQOff + m * L::kOp + ct * 16;
+          if (lane < 8) s_cr[at] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
+          // (dims whose codes are shifted: 2^8 more; they are the second 16 of every 32, lanes 16 on)
+          const float u = lane >= 16 ? up : up * (1.0f / 256.0f);
+          auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * u, __uint_as_float(v & 0xFFFF0000u) * u); };
+          unsigned char* dst = sm + L::kQOff + (step >> 2) * L::kOp + (d0 >> 3) * 2048 + (at & 127) * 16;
 #pragma unroll
-          for (int d = 0; d < HD / 8; ++d) {
-            const float u = ALL || (d & 2) ? up : up * (1.0f / 256.0f);       // (dims whose codes are shifted: 2^8 more)
-            auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * u, __uint_as_float(v & 0xFFFF0000u) * u); };
-            *reinterpret_cast<uint4*>(dst + d * 2048) = make_uint4(half2(q[d].x), half2(q[d].y), half2(q[d].z), half2(q[d].w));
-          }
+          for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(dst + i * 4 * 2048) = make_uint4(half2(q[i].x), half2(q[i].y), half2(q[i].z), half2(q[i].w));
         }
       }
       put(sm + L::kKOff, kr);
       done(&k_full);
-      if (j + 1 < total) { known(j + 1); fetch(P.k, N, kr, N.j0 + ct < N.lim_max); }
+      if (j + 1 < total) { known(j + 1); fetch(P.k, N, kr); }
       if (j > 1) { pga_wait(&v_empty[j & 1], (unsigned)((j >> 1) - 1) & 1u, dead, P.err); __syncwarp(); }
       put(sm + L::kVOff + (j & 1) * L::kOp, vr);
       done(&v_full[j & 1]);
-      if (j + 1 < total) fetch(P.v, N, vr, N.j0 + ct < N.lim_max);
+      if (j + 1 < total) fetch(P.v, N, vr);
     }
   } else if (warp < W_CONV) {
     // ---- softmax ----
-    const int m = warp >> 2, row = tid & 127, bar = 1 + m;
+    const int m = MT == 2 ? warp >> 2 : 0, half = MT == 2 ? 0 : warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_o = tm_o + m * 128 + lanes;
-    constexpr int COLS = 128 / COPIES;            // the positions of a chunk that this copy of the row takes, from col0 on
-    const int part = COPIES == 1 ? 0 : row / RP, col0 = part * COLS;
+    constexpr int COLS = 64 * MT / COPIES;        // the positions of a chunk that this thread takes, from col0 on
+    const int part = COPIES == 1 ? 0 : row / RP, col0 = (part * (MT == 2 ? 1 : 2) + half) * COLS;
+    constexpr int DIMS = MT == 2 ? HD : HD / 2;   // the dims of O that it rescales and writes, from dim0 on
+    const int dim0 = half * DIMS;
     float M = kPgaFloor, l = 0.0f, cr = 0.0f, slope = 0.0f;
     int lim = 0, pos = 0;
     unsigned long long bits = 0;
@@ -369,7 +377,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     for (int j = 0; j < total; ++j) {
       const PtTile& T = info[j % kPtInfo];
       const int b = MT == 2 ? m : (j & 1);
-      const uint32_t t_s = tmem + b * 128 + lanes;
+      const uint32_t t_s = tmem + b * 128 + lanes, t_p = MT == 2 ? t_s : tmem + 384 + b * 64 + lanes;
       pga_wait(&s_full[b], (unsigned)(MT == 2 ? j : (j >> 1)) & 1u, dead, P.err);
       __syncwarp();
       pt_fence_after();
@@ -396,11 +404,11 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           const float a = cr * mt.x;
           pt_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] *= a;
+          for (int i = 0; i < 16; i += 2) { const float2 y = mul2(make_float2(x[i], x[i + 1]), make_float2(a, a)); x[i] = y.x; x[i + 1] = y.y; }
           if (cap) {
             float top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+            for (int i = 0; i < 16; i += 2) top = max3(top, fabsf(x[i]), fabsf(x[i + 1]));
             const float c2 = A.softcap * log2e;
             if (!__any_sync(FULL, !(top <= 0.5f))) {      // tanh y = y (1 - y^2 / 3 + ...): the next term is 9e-8
 #pragma unroll
@@ -464,6 +472,11 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
         }
         pt_wait_ld();
       }
+      if (MT == 1) {                              // both halves of the row's positions have one maximum
+        s_top[j & 1][half][row] = top;
+        pt_sync<1, 256>();
+        top = fmaxf(top, s_top[j & 1][half ^ 1][row]);
+      }
       const bool grow = top > M + kPgaSlack;
       if (__any_sync(FULL, grow)) {
         const float now = grow ? top : M, f = ex2_approx(M - now);
@@ -473,7 +486,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           __syncwarp();
           pt_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < HD; c += 16) {
+          for (int c = dim0; c < dim0 + DIMS; c += 16) {
             float o[16];
             pt_ld16(t_o + c, o);
             pt_wait_ld();
@@ -484,7 +497,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           pt_wait_st();
         }
       }
-      // The weights: those of 32 positions take 16 columns, behind which the scores have been read; the positions of the other copies are zeros.
+      // The weights: those of 32 positions take 16 columns (over scores that have been read); the positions of the other copy are zeros.
       {
         const float Mo = M - kPgaLift;
         float x[2][16];
@@ -510,16 +523,14 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
             s0 = add2(s0, s1);
             l = fmaf(s0.x + s0.y, mt.z, l);
           }
-          pt_st16(t_s + ((col0 + c) >> 1), pk);
+          pt_st16(t_p + ((col0 + c) >> 1), pk);
         }
         pt_wait_ld();
-        if (COPIES > 1) {
+        if (COPIES == 2) {                        // (32 columns of zeros between the two threads of the row)
           uint32_t none[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) none[i] = 0;
-#pragma unroll 1
-          for (int c = 0; c < 64; c += 16)
-            if (c < (col0 >> 1) || c >= (col0 + COLS) >> 1) pt_st16(t_s + c, none);
+          pt_st16(t_p + (part ^ 1) * 32 + half * 16, none);
         }
       }
       pt_wait_st();
@@ -533,55 +544,64 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
         pt_fence_after();
         const int rows = min(RB, T.nq * grp - T.rt * RB), r = m * 128 + row % RP;
         float sum = l, top2 = M, f = 1.0f;
-        if (COPIES > 1) {
-          s_ml[row] = make_float2(M, l);
-          pt_sync(bar);
+        if (MT == 1) {                            // the row's sums: of both halves of the positions, and of its copies
+          s_ml[half][row] = make_float2(M, l);
+          pt_sync<1, 256>();
           sum = 0.0f;
-          for (int k = 0; k < COPIES; ++k) top2 = fmaxf(top2, s_ml[k * RP + row % RP].x);
-          for (int k = 0; k < COPIES; ++k) { const float2 y = s_ml[k * RP + row % RP]; sum += y.y * ex2_approx(y.x - top2); }
+#pragma unroll
+          for (int k = 0; k < COPIES; ++k) top2 = fmaxf(top2, s_ml[0][k * RP + row % RP].x);
+#pragma unroll
+          for (int k = 0; k < COPIES; ++k) {
+            const float2 y = s_ml[0][k * RP + row % RP], z = s_ml[1][k * RP + row % RP];
+            sum += (y.y + z.y) * ex2_approx(y.x - top2);
+          }
           f = ex2_approx(M - top2);
         }
-        const bool whole = T.whole, mine = r < rows && part == 0 && m * 128 + row % RP < RB;
+        const bool whole = T.whole, mine = r < rows && part == 0;
         const int rr = T.rt * RB + r, tok = rr / grp, h = T.kvh * grp + rr - tok * grp;
         const size_t slot = (size_t)(cta * 2 + T.slot) * A.part_rows + r;
-        const float norm = whole ? (sum == 0.0f ? 0.0f : f / sum) : f;
-        const bool nan = whole && !(sum >= 0.0f);
-        float* buf = reinterpret_cast<float*>(sm + L::kEnd);      // [128][17] a block of 16 dims of all copies
+        // (a row that saw nothing is 0; a sum that is not a number leaves its row that way)
+        const float norm = whole ? (sum > 0.0f ? f / sum : (sum == 0.0f ? 0.0f : sum)) : f;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + (long long)(T.q0 + tok) * A.out_stride + (long long)h * HD;
+        const bool vec32 = A.vec_q && (reinterpret_cast<uintptr_t>(out) & 31) == 0;
+        float* buf = reinterpret_cast<float*>(sm + L::kEnd) + half * 64 * 17;      // MT = 1: [64][17] a block of 16 dims of the second copies
 #pragma unroll 1
-        for (int c = 0; c < HD; c += 16) {
+        for (int c = dim0; c < dim0 + DIMS; c += 16) {
           float o[16];
           pt_ld16(t_o + c, o);
           pt_wait_ld();
-          const float g = ALL || (c & 16) ? norm * 256.0f : norm;          // (the shifted dims)
+          const float g = c & 16 ? norm * 256.0f : norm;          // (the shifted dims)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = nan ? sum : o[i] * g;
-          if (COPIES > 1) {
-            if (part > 0)
+          for (int i = 0; i < 16; ++i) o[i] *= g;
+          if (COPIES == 2) {
+            if (part == 1)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) buf[row * 17 + i] = o[i];
-            pt_sync(bar);
+              for (int i = 0; i < 16; ++i) buf[(row - RP) * 17 + i] = o[i];
+            if (half == 0) pt_sync<2, 128>(); else pt_sync<3, 128>();
             if (part == 0)
-              for (int k = 1; k < COPIES; ++k)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] += buf[(k * RP + row) * 17 + i];
-            pt_sync(bar);
+              for (int i = 0; i < 16; ++i) o[i] += buf[row * 17 + i];
+            if (half == 0) pt_sync<2, 128>(); else pt_sync<3, 128>();
           }
           if (mine) {
             if (whole) {
-              if (sum == 0.0f)
+              if (vec32) {
+                uint32_t u[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] = 0.0f;
-              __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + (long long)(T.q0 + tok) * A.out_stride + (long long)h * HD + c;
-              store8(out, A.vec_q, *reinterpret_cast<float (*)[8]>(o));
-              store8(out + 8, A.vec_q, *reinterpret_cast<float (*)[8]>(o + 8));
+                for (int i = 0; i < 8; ++i) u[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+                stg32(out + c, u);
+              } else {
+                store8(out + c, A.vec_q, *reinterpret_cast<float (*)[8]>(o));
+                store8(out + c + 8, A.vec_q, *reinterpret_cast<float (*)[8]>(o + 8));
+              }
             } else {
-              float4* d = reinterpret_cast<float4*>(A.part + slot * HD + c);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+              uint32_t* d = reinterpret_cast<uint32_t*>(A.part + slot * HD + c);
+              stg32(d, reinterpret_cast<const uint32_t*>(o));
+              stg32(d + 8, reinterpret_cast<const uint32_t*>(o) + 8);
             }
           }
         }
-        if (mine && !whole) *reinterpret_cast<float2*>(A.part_ml + slot * 2) = make_float2(top2, sum);
+        if (mine && !whole && half == 0) *reinterpret_cast<float2*>(A.part_ml + slot * 2) = make_float2(top2, sum);
         if (tid == 0 && !whole) A.desc[cta * 2 + T.slot] = make_int4(1 | (T.to_end ? 2 : 0), T.e, T.kvh, T.rt);
         pt_fence_before();
       }

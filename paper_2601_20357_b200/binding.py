@@ -380,22 +380,20 @@ class Tabed:
         return int(lib().tabed_launch_count(self._h))
 
 
-def _rows(t: torch.Tensor, dtype, n: int, heads: int, hd: int, name: str, device: torch.device) -> int:
-    """Pointer of rows [n][heads][hd] that are whole in themselves (stride(0) apart)."""
-    if t.dtype != dtype:
+def _rows(t: torch.Tensor, dtype, n: int, heads: int, hd: int, name: str, device: torch.device):
+    """Pointer of rows [n][heads][hd] that are whole in themselves, and the elements between them (of one row, its length)."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != (n, heads, hd):
+    if t.shape != (n, heads, hd):
         raise ValueError(f"{name}: expected shape {(n, heads, hd)}, got {tuple(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd) or (n > 1 and t.stride(0) < heads * hd):
+    row, head, one = t.stride()
+    if n < 2:
+        row = heads * hd
+    if one != 1 or (head != hd and heads > 1) or row < heads * hd:
         raise ValueError(f"{name}: heads and values of a row must be contiguous, rows must not overlap")
     if t.device != device:
         raise ValueError(f"{name}: expected device {device}, got {t.device}")
-    return t.data_ptr()
-
-
-def _stride(t: torch.Tensor) -> int:
-    """Elements between rows; of one row, its length."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), row
 
 
 _PAGES_DTYPE = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
@@ -470,8 +468,9 @@ class Pages:
         t = TabedPagesNew()
         t.layer, t.n, t.n_tokens, t.max_new, t.dtype = layer, n, T, max_new, _PAGES_DTYPE[k.dtype]
         t.seq, t.first, t.start = _ptr(seq, i, n, "seq", d), _ptr(first, i, n + 1, "first", d), _ptr(start, i, n, "start", d)
-        t.k, t.v, t.kv_stride = _rows(k, k.dtype, T, self.Hkv, self.hd, "k", d), _rows(v, k.dtype, T, self.Hkv, self.hd, "v", d), _stride(k)
-        if _stride(v) != t.kv_stride:
+        t.k, t.kv_stride = _rows(k, k.dtype, T, self.Hkv, self.hd, "k", d)
+        t.v, stride = _rows(v, k.dtype, T, self.Hkv, self.hd, "v", d)
+        if stride != t.kv_stride:
             raise ValueError("v: rows must be as far apart as those of k")
         if positions is not None:
             t.n_axes = len(sections)
@@ -484,8 +483,9 @@ class Pages:
             if positions is None or q_out is None:
                 raise ValueError("q: needs positions and q_out")
             H = q.shape[1]
-            t.q, t.q_out, t.n_heads = _rows(q, k.dtype, T, H, self.hd, "q", d), _rows(q_out, k.dtype, T, H, self.hd, "q_out", d), H
-            t.q_stride, t.q_out_stride = _stride(q), _stride(q_out)
+            t.n_heads = H
+            t.q, t.q_stride = _rows(q, k.dtype, T, H, self.hd, "q", d)
+            t.q_out, t.q_out_stride = _rows(q_out, k.dtype, T, H, self.hd, "q_out", d)
         _check(lib().tabed_pages_append(self._ref, C.byref(t)), "tabed_pages_append")
 
     def attention(self, layer: int, q: torch.Tensor, out: torch.Tensor, seq: Optional[torch.Tensor], first: torch.Tensor, length: torch.Tensor,
@@ -499,8 +499,8 @@ class Pages:
         t = TabedPagesQuery()
         t.layer, t.n, t.n_tokens, t.max_new, t.dtype, t.n_heads = layer, n, T, max_new, _PAGES_DTYPE[q.dtype], H
         t.seq, t.first, t.length = _ptr(seq, i, n, "seq", d), _ptr(first, i, n + 1, "first", d), _ptr(length, i, n, "length", d)
-        t.q, t.q_stride = _rows(q, q.dtype, T, H, self.hd, "q", d), _stride(q)
-        t.out, t.out_stride = _rows(out, q.dtype, T, H, self.hd, "out", d), _stride(out)
+        t.q, t.q_stride = _rows(q, q.dtype, T, H, self.hd, "q", d)
+        t.out, t.out_stride = _rows(out, q.dtype, T, H, self.hd, "out", d)
         t.scale, t.softcap = scale, softcap
         t.slopes, t.prefix = _ptr(slopes, torch.float32, H, "slopes", d), _ptr(prefix, i, n, "prefix", d)
         if tree is not None:

@@ -91,16 +91,23 @@ int sm_count(int dev) {
 // rows of `heads` heads of `hd` values of `esz` bytes, `stride` values apart, start on 16-byte boundaries
 bool rows_aligned(const void* p, long long stride, size_t esz) { return aligned(p, 16) && (stride * (long long)esz) % 16 == 0; }
 
-template <typename T>
-int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, bool small, size_t smem) {
-  if (small) return launch(p, k_pages_append<T, 32, 2>, grid, kAppendThreads, smem, a);
-  auto kern = k_pages_append<T, kAppendThreads, 4>;
+template <typename T, int MAXI>
+int launch_append_long(const tabed_pages* p, const AppendArgs& a, dim3 grid, size_t smem) {
+  auto kern = k_pages_append<T, kAppendThreads, MAXI>;
   static bool set[kMaxDevices] = {false};
   if (!set[p->device]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 64 * (int)sizeof(float2)) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAXI * kAppendThreads * 4 * (int)sizeof(float4)) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
     set[p->device] = true;
   }
   return launch(p, kern, grid, kAppendThreads, smem, a);
+}
+
+// items: of 8 rotated pairs, that a head's tokens of a block are at most
+template <typename T>
+int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, int items, size_t smem) {
+  if (items <= 32) return launch(p, k_pages_append<T, 32, 1>, grid, kAppendThreads, smem, a);
+  if (items <= kAppendThreads) return launch_append_long<T, 1>(p, a, grid, smem);
+  return items <= 2 * kAppendThreads ? launch_append_long<T, 2>(p, a, grid, smem) : launch_append_long<T, 4>(p, a, grid, smem);
 }
 
 template <int HD, bool TWO, bool R8>
@@ -214,8 +221,9 @@ int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t) {
     for (int i = 0; i < half; ++i) a.turns[i] = pow((double)t->theta, -2.0 * i / hd) / 6.283185307179586476925;
   const int ps = p->page_tokens, most = std::min(t->max_new, ps);      // tokens of a block
   a.nblk = (t->max_new + ps - 2) / ps + 1;
-  // Units of a warp where a head's tokens of a block are at most 64 items of 8 pairs (a token of 128 values has 8 of them)
-  const bool small = most * (hd / 16) <= 64;
+  // Units of a warp where a head's tokens of a block are one item a lane (a token of 128 values has 8 of them)
+  const int items = most * (hd / 16);
+  const bool small = items <= 32;
   const int heads = 2 * p->n_kv_heads + (with_q ? t->n_heads : 0);
   const long long blocks = (long long)t->n * a.nblk;
   if (blocks > 0x7FFFFFFFll) return TABED_ERR_UNSUPPORTED;
@@ -224,9 +232,9 @@ int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t) {
   int groups = (int)std::min<long long>((heads + per - 1) / per, std::max<long long>(1, (8ll * sm_count(p->device) + blocks - 1) / blocks));
   a.hpc = ((heads + groups - 1) / groups + per - 1) / per * per;
   groups = (heads + a.hpc - 1) / a.hpc;
-  const size_t smem = t->n_axes > 0 ? (size_t)most * half * sizeof(float2) : 0;
+  const size_t smem = t->n_axes > 0 ? (size_t)items * 4 * sizeof(float4) : 0;
   const dim3 grid((unsigned)blocks, (unsigned)groups);
-  return t->dtype == TABED_DTYPE_FP32 ? launch_append<float>(p, a, grid, small, smem) : launch_append<__nv_bfloat16>(p, a, grid, small, smem);
+  return t->dtype == TABED_DTYPE_FP32 ? launch_append<float>(p, a, grid, items, smem) : launch_append<__nv_bfloat16>(p, a, grid, items, smem);
 }
 
 int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {

@@ -117,15 +117,46 @@ __device__ __forceinline__ bool named_twice(const int* seq, int e, int n) {
 
 constexpr int kAppendThreads = 256;
 
+// eight values as they lie in memory: asked for early, turned into fp32 late
+template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8(const T* p, bool vec) {
+  Raw8<T> r;
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  } else {
+    uint32_t w[4 * (sizeof(T) / 2)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else if (i % 2 == 0) w[i / 2] = reinterpret_cast<const unsigned short*>(p)[i] | (uint32_t)reinterpret_cast<const unsigned short*>(p)[i + 1] << 16;
+    }
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+  return r;
+}
+__device__ __forceinline__ void open8(const Raw8<__nv_bfloat16>& r, float (&f)[8]) {
+  const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void open8(const Raw8<float>& r, float (&f)[8]) {
+  const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+}
+
 // A CTA has one block of page_tokens tokens of one entry and hpc of the K, V and query heads: the cosines and sines of
 // its tokens are taken once (the angle's turns in fp64: positions of any size) and serve all of those heads.  A unit (a head's
 // tokens of the block) is worked by TPU threads, each with up to MAXI items of 8 rotated pairs in registers between the
-// block's maximum and the rounding: k, v and q are read once.  Short units (single tokens) take a warp each, 8 at once;
-// long ones the whole CTA.
+// block's maximum and the rounding: k, v and q are read once, the next unit's while this one is worked.  Short units (single
+// tokens) take a warp each, 8 at once; long ones the whole CTA.
 template <typename T, int TPU, int MAXI>
 __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArgs A) {
-  extern __shared__ float2 ap_cs[];               // [tokens of the block][hd / 2] cosine, sine
-  __shared__ float s_red[kAppendThreads / 32];
+  extern __shared__ float4 ap_cs[];               // [4][items] cosine and sine of two frequencies: the lanes' places are neighbours
+  __shared__ float s_red[2][kAppendThreads / 32];
   const PagesDev& P = A.P;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int e = blockIdx.x / A.nblk, slot = blockIdx.x - e * A.nblk;
@@ -140,23 +171,47 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
     if (tid == 0) atomicOr(P.err, PERR_KV);
     return;
   }
-  const int p1 = p0 + (f1 - f0), bi = p0 / ps + slot;
+  const int p1 = p0 + (f1 - f0), bi = (p0 >> P.ls) + slot;
   if (f1 == f0 || bi * ps >= p1) return;
   const int lo = max(p0, bi * ps), cnt = min(p1, (bi + 1) * ps) - lo, off = lo - bi * ps, t0 = f0 + (lo - p0);
+  const int u0 = blockIdx.y * A.hpc, u1 = min(u0 + A.hpc, 2 * P.Hkv + (A.has_q ? A.n_heads : 0));
+  const int lt = 31 - __clz(hd >> 4), n_items = cnt << lt;      // hd / 16 = 2^lt items a token
+  constexpr int UNITS = kAppendThreads / TPU;
+  const int me = TPU == 32 ? lane : tid;
+  Raw8<T> ra[MAXI], rb[MAXI];
+  auto ask = [&](int u) {                         // unit u's values
+    const bool is_q = u >= 2 * P.Hkv, is_v = !is_q && u >= P.Hkv;
+    const T* in = reinterpret_cast<const T*>(is_q ? A.q : (is_v ? A.v : A.k)) + (size_t)(is_q ? u - 2 * P.Hkv : (is_v ? u - P.Hkv : u)) * hd;
+    const long long stride = is_q ? A.q_stride : A.kv_stride;
+    const bool vec = is_q ? A.vec_q : A.vec_kv;
+#pragma unroll
+    for (int j = 0; j < MAXI; ++j) {
+      const int it = me + j * TPU;
+      if (it < n_items) {
+        const T* row = in + (long long)(t0 + (it >> lt)) * stride + (it & ((1 << lt) - 1)) * 8;
+        ra[j] = raw8(row, vec);
+        rb[j] = raw8(row + half, vec);
+      }
+    }
+  };
+  int u = u0 + (TPU == 32 ? warp : 0);
+  if (u < u1) ask(u);
   const int page = P.table[(size_t)s * P.max_pages + bi];
   bool own = page >= 0 && page < P.NP;
   if (own) own = P.ref[page] == 1;
-  const int u0 = blockIdx.y * A.hpc, u1 = min(u0 + A.hpc, 2 * P.Hkv + (A.has_q ? A.n_heads : 0));
   if (A.n_axes) {
-    for (int i = tid; i < cnt * half; i += kAppendThreads) {
-      const int tok = i / half, f = i - tok * half;
-      int axis = 0, upto = A.sections[0];
-      while (f >= upto && axis < A.n_axes - 1) upto += A.sections[++axis];
-      double turn = (double)A.positions[(size_t)axis * A.n_tokens + t0 + tok] * A.turns[f];
-      turn -= rint(turn);
-      float sn, cs;
-      sincospif((float)(2.0 * turn), &sn, &cs);
-      ap_cs[i] = make_float2(cs, sn);
+    for (int i = tid; i < n_items * 4; i += kAppendThreads) {
+      const int k = i / n_items, it = i - k * n_items, tok = it >> lt, f = (it & ((1 << lt) - 1)) * 8 + 2 * k;
+      float c[4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        int axis = 0, upto = A.sections[0];
+        while (f + x >= upto && axis < A.n_axes - 1) upto += A.sections[++axis];
+        double turn = (double)A.positions[(size_t)axis * A.n_tokens + t0 + tok] * A.turns[f + x];
+        turn -= rint(turn);
+        sincospif((float)(2.0 * turn), &c[2 * x + 1], &c[2 * x]);
+      }
+      ap_cs[i] = make_float4(c[0], c[1], c[2], c[3]);
     }
   }
   if (A.seq && named_twice(A.seq, e, A.n)) {      // (a barrier, too)
@@ -165,52 +220,47 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
   }
   __syncthreads();
   if (!own && tid == 0) atomicOr(P.err, PGERR_INVALID);
-  const int per_tok = hd >> 4, n_items = cnt * per_tok;
-  constexpr int UNITS = kAppendThreads / TPU;
-  const int me = TPU == 32 ? lane : tid;
-  for (int u = u0 + (TPU == 32 ? warp : 0); u < u1; u += UNITS) {
+  for (int n = 0; u < u1; u += UNITS, n ^= 1) {
     const bool is_q = u >= 2 * P.Hkv, is_v = !is_q && u >= P.Hkv;
-    if (!is_q && !own) continue;
     const int head = is_q ? u - 2 * P.Hkv : (is_v ? u - P.Hkv : u);
-    const T* in = reinterpret_cast<const T*>(is_q ? A.q : (is_v ? A.v : A.k)) + (size_t)head * hd;
-    const long long stride = is_q ? A.q_stride : A.kv_stride;
-    const bool vec = is_q ? A.vec_q : A.vec_kv, turned = A.n_axes && !is_v;
+    const bool turned = A.n_axes && !is_v;
     float x[MAXI][16], amax = 0.0f;
     bool odd = false;
 #pragma unroll
     for (int j = 0; j < MAXI; ++j) {
       const int it = me + j * TPU;
-      if (it >= n_items) break;
-      const int tok = it / per_tok, c = it - tok * per_tok;
-      const T* row = in + (long long)(t0 + tok) * stride + c * 8;
-      float a[8], b[8];
-      load8(row, vec, a);
-      load8(row + half, vec, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float y = a[i], z = b[i];
+      if (it < n_items) {
+        float a[8], b[8];
+        open8(ra[j], a);
+        open8(rb[j], b);
         if (turned) {
-          const float2 cs = ap_cs[tok * half + c * 8 + i];
-          y = a[i] * cs.x - b[i] * cs.y;
-          z = b[i] * cs.x + a[i] * cs.y;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 cs = ap_cs[k * n_items + it];
+            const int i = 2 * k;
+            const float y0 = a[i] * cs.x - b[i] * cs.y, y1 = a[i + 1] * cs.z - b[i + 1] * cs.w;
+            b[i] = b[i] * cs.x + a[i] * cs.y;
+            b[i + 1] = b[i + 1] * cs.z + a[i + 1] * cs.w;
+            a[i] = y0; a[i + 1] = y1;
+          }
         }
-        x[j][i] = y; x[j][8 + i] = z;
-      }
-      if (is_q) {
-        T* o = reinterpret_cast<T*>(A.q_out) + (size_t)head * hd + (long long)(t0 + tok) * A.q_out_stride + c * 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { a[i] = x[j][i]; b[i] = x[j][8 + i]; }
-        store8(o, vec, a);
-        store8(o + half, vec, b);
-      } else {
+        for (int i = 0; i < 8; ++i) { x[j][i] = a[i]; x[j][8 + i] = b[i]; }
+        if (is_q) {
+          T* o = reinterpret_cast<T*>(A.q_out) + (size_t)head * hd + (long long)(t0 + (it >> lt)) * A.q_out_stride + (it & ((1 << lt) - 1)) * 8;
+          store8(o, A.vec_q, a);
+          store8(o + half, A.vec_q, b);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float m = fabsf(x[j][i]);
-          if (m < INFINITY) amax = fmaxf(amax, m); else odd = true;
+          for (int i = 0; i < 16; ++i) {
+            const float m = fabsf(x[j][i]);
+            if (m < INFINITY) amax = fmaxf(amax, m); else odd = true;
+          }
         }
       }
     }
-    if (is_q) continue;
+    if (u + UNITS < u1) ask(u + UNITS);
+    if (is_q || !own) continue;                   // (the same for all threads of the unit)
     const size_t at = ((size_t)A.layer * P.NP + page) * P.Hkv + head;
     float* scale = (is_v ? P.v_scale : P.k_scale) + at;
     uint8_t* codes = (is_v ? P.v : P.k) + at * ps * hd;
@@ -218,12 +268,13 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     if (TPU > 32) {
-      if (lane == 0) s_red[warp] = amax;
-      __syncthreads();
-      amax = s_red[lane & 7];
+      if (lane == 0) s_red[n][warp] = amax;
+      __syncthreads();                            // (everybody has read the old scale, too)
+      amax = s_red[n][lane & 7];
 #pragma unroll
       for (int o = 4; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      __syncthreads();                            // (everybody has read the old scale, and the next unit may use s_red)
+    } else {
+      __syncwarp();
     }
     const float now = fmaxf(least_scale(amax), old), inv = 1.0f / now;
     if (me == 0) *scale = now;
@@ -241,14 +292,14 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
 #pragma unroll
     for (int j = 0; j < MAXI; ++j) {
       const int it = me + j * TPU;
-      if (it >= n_items) break;
-      const int tok = it / per_tok, c = it - tok * per_tok;
-      uint8_t* row = codes + (size_t)(off + tok) * hd + c * 8;
-      float y[16];
+      if (it < n_items) {
+        uint8_t* row = codes + (size_t)(off + (it >> lt)) * hd + (it & ((1 << lt) - 1)) * 8;
+        float y[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = x[j][i] != x[j][i] ? 0.0f : x[j][i] * inv;     // (the conversion saturates)
-      *reinterpret_cast<uint2*>(row) = make_uint2(to_e4m3x4(y[0], y[1], y[2], y[3]), to_e4m3x4(y[4], y[5], y[6], y[7]));
-      *reinterpret_cast<uint2*>(row + half) = make_uint2(to_e4m3x4(y[8], y[9], y[10], y[11]), to_e4m3x4(y[12], y[13], y[14], y[15]));
+        for (int i = 0; i < 16; ++i) y[i] = x[j][i] != x[j][i] ? 0.0f : x[j][i] * inv;     // (the conversion saturates)
+        *reinterpret_cast<uint2*>(row) = make_uint2(to_e4m3x4(y[0], y[1], y[2], y[3]), to_e4m3x4(y[4], y[5], y[6], y[7]));
+        *reinterpret_cast<uint2*>(row + half) = make_uint2(to_e4m3x4(y[8], y[9], y[10], y[11]), to_e4m3x4(y[12], y[13], y[14], y[15]));
+      }
     }
   }
 }

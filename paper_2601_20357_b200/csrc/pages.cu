@@ -91,23 +91,23 @@ int sm_count(int dev) {
 // rows of `heads` heads of `hd` values of `esz` bytes, `stride` values apart, start on 16-byte boundaries
 bool rows_aligned(const void* p, long long stride, size_t esz) { return aligned(p, 16) && (stride * (long long)esz) % 16 == 0; }
 
-template <typename T, int MAXI>
+template <typename T, int THREADS, int MAXI>
 int launch_append_long(const tabed_pages* p, const AppendArgs& a, dim3 grid, size_t smem) {
-  auto kern = k_pages_append<T, kAppendThreads, MAXI>;
+  auto kern = k_pages_append<T, THREADS, MAXI>;
   static bool set[kMaxDevices] = {false};
   if (!set[p->device]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAXI * kAppendThreads * 4 * (int)sizeof(float4)) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAXI * THREADS * 4 * (int)sizeof(float4)) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
     set[p->device] = true;
   }
-  return launch(p, kern, grid, kAppendThreads, smem, a);
+  return launch(p, kern, grid, THREADS, smem, a);
 }
 
 // items: of 8 rotated pairs, that a head's tokens of a block are at most
 template <typename T>
 int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, int items, size_t smem) {
   if (items <= 32) return launch(p, k_pages_append<T, 32, 1>, grid, kAppendThreads, smem, a);
-  if (items <= kAppendThreads) return launch_append_long<T, 1>(p, a, grid, smem);
-  return items <= 2 * kAppendThreads ? launch_append_long<T, 2>(p, a, grid, smem) : launch_append_long<T, 4>(p, a, grid, smem);
+  if (items <= 256) return launch_append_long<T, 256, 1>(p, a, grid, smem);
+  return items <= 512 ? launch_append_long<T, 512, 1>(p, a, grid, smem) : launch_append_long<T, 512, 2>(p, a, grid, smem);
 }
 
 template <int HD, bool TWO, bool R8>
@@ -285,7 +285,15 @@ int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t*
   if (!guard.ok) return TABED_ERR_CUDA;
   CompactArgs a;
   a.P = on_device(p); a.seq = seq; a.start = start; a.count = count; a.index = index; a.n = n; a.width = width;
-  return launch(p, k_pages_compact, dim3(n, p->n_layers, 2 * p->n_kv_heads), kCompactThreads, 0, a);
+  // A warp a unit where there are many units or few tokens, else four; blocks of more than 4 KB take four.  1024 of 4096 tokens, 8 sequences, 4
+  // layers, 12 heads (768 units): one warp 55 us, four 40; the 6 tokens of 32 trees, 12 layers, 2 heads (1536 units): one 10.2.
+  const int bytes = p->page_tokens * p->head_dim;
+  const bool one = bytes <= 4096 && (width < p->page_tokens || (long long)n * p->n_layers * 2 * p->n_kv_heads > 32ll * sm_count(p->device));
+  const int per = kCompactThreads / 32 / (one ? 1 : 4);
+  const dim3 grid(n, p->n_layers, (2 * p->n_kv_heads + per - 1) / per);
+  if (one) return launch(p, k_pages_compact<1, 8>, grid, kCompactThreads, 0, a);
+  if (bytes <= 4096) return launch(p, k_pages_compact<4, 2>, grid, kCompactThreads, 0, a);
+  return bytes <= 8192 ? launch(p, k_pages_compact<4, 4>, grid, kCompactThreads, 0, a) : launch(p, k_pages_compact<4, 8>, grid, kCompactThreads, 0, a);
 }
 
 int tabed_pages_last_error(const tabed_pages* p) {

@@ -152,11 +152,13 @@ __device__ __forceinline__ void open8(const Raw8<float>& r, float (&f)[8]) {
 // its tokens are taken once (the angle's turns in fp64: positions of any size) and serve all of those heads.  A unit (a head's
 // tokens of the block) is worked by TPU threads, each with up to MAXI items of 8 rotated pairs in registers between the
 // block's maximum and the rounding: k, v and q are read once, the next unit's while this one is worked.  Short units (single
-// tokens) take a warp each, 8 at once; long ones the whole CTA.
+// tokens) take a warp each, 8 at once; long ones the whole CTA, of 256 or 512 threads: an item a thread keeps most warps on an SM (64
+// tokens of 128 values: two items on 256 threads 144 us, one on 512 112 us, at 18,800 tokens of 48 heads).
 template <typename T, int TPU, int MAXI>
-__global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArgs A) {
+__global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 && MAXI == 1 ? 2 : 1) k_pages_append(const AppendArgs A) {
   extern __shared__ float4 ap_cs[];               // [4][items] cosine and sine of two frequencies: the lanes' places are neighbours
-  __shared__ float s_red[2][kAppendThreads / 32];
+  constexpr int THREADS = TPU == 32 ? kAppendThreads : TPU, WARPS = THREADS / 32;
+  __shared__ float s_red[2][WARPS];
   const PagesDev& P = A.P;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int e = blockIdx.x / A.nblk, slot = blockIdx.x - e * A.nblk;
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
   const int lo = max(p0, bi * ps), cnt = min(p1, (bi + 1) * ps) - lo, off = lo - bi * ps, t0 = f0 + (lo - p0);
   const int u0 = blockIdx.y * A.hpc, u1 = min(u0 + A.hpc, 2 * P.Hkv + (A.has_q ? A.n_heads : 0));
   const int lt = 31 - __clz(hd >> 4), n_items = cnt << lt;      // hd / 16 = 2^lt items a token
-  constexpr int UNITS = kAppendThreads / TPU;
+  constexpr int UNITS = THREADS / TPU;
   const int me = TPU == 32 ? lane : tid;
   Raw8<T> ra[MAXI], rb[MAXI];
   auto ask = [&](int u) {                         // unit u's values
@@ -200,7 +202,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
   bool own = page >= 0 && page < P.NP;
   if (own) own = P.ref[page] == 1;
   if (A.n_axes) {
-    for (int i = tid; i < n_items * 4; i += kAppendThreads) {
+    for (int i = tid; i < n_items * 4; i += THREADS) {
       const int k = i / n_items, it = i - k * n_items, tok = it >> lt, f = (it & ((1 << lt) - 1)) * 8 + 2 * k;
       float c[4];
 #pragma unroll
@@ -270,9 +272,9 @@ __global__ void __launch_bounds__(kAppendThreads) k_pages_append(const AppendArg
     if (TPU > 32) {
       if (lane == 0) s_red[n][warp] = amax;
       __syncthreads();                            // (everybody has read the old scale, too)
-      amax = s_red[n][lane & 7];
+      amax = s_red[n][lane & (WARPS - 1)];
 #pragma unroll
-      for (int o = 4; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      for (int o = WARPS / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     } else {
       __syncwarp();
     }
@@ -479,105 +481,116 @@ struct CompactArgs {
 constexpr int kCompactThreads = 256;
 constexpr int kCompactTile = 1024;        // tokens whose places are looked up at once (a multiple of page_tokens)
 
-// A CTA has one entry, layer and KV head of K or V and fills the target blocks one by one.  Sources lie at or behind their
-// targets in ascending order, so no source of a block lies in a block filled before it; the reads of a block and its writes are
-// parted by the barriers of the scale's maximum, and the next block's reads are on their way meanwhile.
-// grid (n, L, 2 Hkv)
+// A CTA has one entry and layer and up to 8 units (a KV head of K or V), each worked by UW warps that fill its target blocks one by one; the
+// places of the tokens are looked up once for all of them.  Sources lie at or behind their targets in ascending order, so no source of a block lies in a
+// block filled before it: reads may run ahead at will (two blocks here), and a block's reads and writes are parted by the maximum of its scales.
+// MAXV: 16-byte pieces of a block per thread.  Bound by the instructions and trips to memory of a unit's blocks, one after the other.
+// grid (n, L, ceil(2 Hkv UW / 8))
+template <int UW, int MAXV>
 __global__ void __launch_bounds__(kCompactThreads) k_pages_compact(const CompactArgs A) {
   const PagesDev& P = A.P;
-  const int e = blockIdx.x, layer = blockIdx.y, head = blockIdx.z >> 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const bool is_v = blockIdx.z & 1;
-  __shared__ long long s_src[kCompactTile];     // a token's page * page_tokens + its place in the page
+  constexpr int UNITS = kCompactThreads / 32 / UW, TPU = 32 * UW;
+  const int e = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, mine = warp / UW, me = tid - mine * TPU;
+  const int unit = blockIdx.z * UNITS + mine, head = unit >> 1;
+  const bool is_v = unit & 1, there = unit < 2 * P.Hkv;
+  __shared__ int2 s_src[kCompactTile];            // a token's page, and its place in the page
   __shared__ float s_red[2][kCompactThreads / 32];
   pdl_trigger();
   pdl_wait();
-  const int s = A.seq[e], start = A.start[e], count = A.count[e], ps = P.ps, hd = P.hd, cap = P.max_pages * ps;
+  const int s = A.seq[e], start = A.start[e], count = A.count[e], ps = P.ps, ls = P.ls, hd = P.hd, cap = P.max_pages * ps;
   const int* index = A.index + (size_t)e * A.width;
   int bad = s < 0 || s >= P.n_seqs || start < 0 || count < 0 || count > A.width || start > cap - count;
   const int* table = P.table + (size_t)(bad ? 0 : s) * P.max_pages;
+  // places of the tokens i0 .. of the next tile
+  int tile0 = 0;
+  auto look_up = [&](int i0) {
+    tile0 = i0;
+    for (int i = tid; i < kCompactTile && i0 + i < count; i += kCompactThreads) {
+      const int x = index[i0 + i];
+      s_src[i] = make_int2(table[x >> ls], x & (ps - 1));
+    }
+    __syncthreads();
+  };
   if (!bad) {
     for (int i = tid; i < count; i += kCompactThreads) {
       const int x = index[i];
       int wrong = x < start + i || x >= cap || (i > 0 && index[i - 1] >= x);
-      if (!wrong) { const int pg = table[x / ps]; wrong = pg < 0 || pg >= P.NP; }
+      if (!wrong) {
+        const int pg = table[x >> ls];
+        wrong = pg < 0 || pg >= P.NP;
+        if (i < kCompactTile) s_src[i] = make_int2(pg, x & (ps - 1));
+      }
       bad |= wrong;
     }
     if (count > 0)
-      for (int b = start / ps + tid; b <= (start + count - 1) / ps; b += kCompactThreads) {
+      for (int b = (start >> ls) + tid; b <= (start + count - 1) >> ls; b += kCompactThreads) {
         const int pg = table[b];
         bad |= pg < 0 || pg >= P.NP || P.ref[pg] != 1;
       }
+    for (int i = tid; i < A.n; i += kCompactThreads) bad |= i != e && A.seq[i] == s;      // (named twice)
   }
-  bad = __syncthreads_or(bad);
-  bad |= named_twice(A.seq, e, A.n);
-  if (bad) {
+  if (__syncthreads_or(bad)) {
     if (tid == 0) atomicOr(P.err, PGERR_INVALID);
     return;
   }
   if (count == 0) return;
-  uint8_t* codes = (is_v ? P.v : P.k) + ((size_t)layer * P.NP * P.Hkv + head) * ps * hd;        // + page * Hkv * ps * hd
-  float* scale = (is_v ? P.v_scale : P.k_scale) + (size_t)layer * P.NP * P.Hkv + head;          // + page * Hkv
+  uint8_t* codes = (is_v ? P.v : P.k) + ((size_t)layer * P.NP * P.Hkv + (there ? head : 0)) * ps * hd;        // + page * Hkv * ps * hd
+  float* scale = (is_v ? P.v_scale : P.k_scale) + (size_t)layer * P.NP * P.Hkv + (there ? head : 0);          // + page * Hkv
   const size_t page_codes = (size_t)P.Hkv * ps * hd;
-  const int vec_tok = hd >> 4;
-  constexpr int MAXV = 4;                       // 16-byte pieces of a block per thread: 128 tokens of 128 bytes
-  uint4 now[MAXV], next[MAXV];
-  float now_s[MAXV], next_s[MAXV];
+  const int lv = 31 - __clz(hd >> 4);             // 16-byte pieces of a token: 2^lv
   // first token (of the entry's moved ones), tokens and place of target block b
   auto span = [&](int b, int& i0, int& cnt, int& off) {
-    const int lo = max(start, b * ps), hi = min(start + count, (b + 1) * ps);
-    i0 = lo - start; cnt = hi - lo; off = lo - b * ps;
+    const int lo = max(start, b << ls), hi = min(start + count, (b + 1) << ls);
+    i0 = lo - start; cnt = hi - lo; off = lo - (b << ls);
   };
-  int tile0 = 0;
-  auto look_up = [&](int i0) {                  // places of the tokens i0 .. of the next tile
-    tile0 = i0;
-    for (int i = tid; i < kCompactTile && i0 + i < count; i += kCompactThreads) {
-      const int x = index[i0 + i];
-      s_src[i] = (long long)table[x / ps] * ps + x % ps;
-    }
-    __syncthreads();
-  };
-  auto fetch = [&](int i0, int cnt, uint4 (&w)[MAXV], float (&ws)[MAXV]) {
+  struct Block { uint4 w[MAXV]; float s[MAXV]; };
+  auto fetch = [&](int b, Block& B) {
+    int i0, cnt, off;
+    span(b, i0, cnt, off);
 #pragma unroll
     for (int j = 0; j < MAXV; ++j) {
-      const int x = tid + j * kCompactThreads;
-      ws[j] = 0.0f;
-      if (x < cnt * vec_tok) {
-        const int tok = x / vec_tok;
-        const long long at = s_src[i0 - tile0 + tok], page = at / ps, row = at - page * ps;
-        w[j] = *reinterpret_cast<const uint4*>(codes + page * page_codes + row * hd + ((x - tok * vec_tok) << 4));
-        ws[j] = scale[page * P.Hkv];
+      const int x = me + j * TPU;
+      B.s[j] = 0.0f;
+      if (there && x < cnt << lv) {
+        const int2 at = s_src[i0 - tile0 + (x >> lv)];
+        B.w[j] = *reinterpret_cast<const uint4*>(codes + at.x * page_codes + at.y * hd + ((x & ((1 << lv) - 1)) << 4));
+        B.s[j] = scale[(size_t)at.x * P.Hkv];
       }
     }
   };
-  const int b0 = start / ps, b1 = (start + count - 1) / ps;
-  int i0, cnt, off;
-  span(b0, i0, cnt, off);
-  look_up(0);
-  fetch(i0, cnt, now, now_s);
-  for (int b = b0; b <= b1; ++b) {
-    int ni0 = 0, ncnt = 0, noff = 0;
-    if (b < b1) {
-      span(b + 1, ni0, ncnt, noff);
-      if (ni0 + ncnt > tile0 + kCompactTile) { __syncthreads(); look_up(ni0); }
-      fetch(ni0, ncnt, next, next_s);
-    }
+  const int b0 = start >> ls, b1 = (start + count - 1) >> ls;
+  int known = b0;                                 // blocks before this one have been asked for
+  auto ask = [&](Block& B) {                      // the next block's values; the whole CTA comes here together
+    if (known > b1) return;
+    int i0, cnt, off;
+    span(known, i0, cnt, off);
+    if (i0 + cnt > tile0 + kCompactTile) { __syncthreads(); look_up(i0); }
+    fetch(known++, B);
+  };
+  auto settle = [&](int b, const Block& B) {
+    int i0, cnt, off;
+    span(b, i0, cnt, off);
     const int page = table[b];
-    const float old = off > 0 ? scale[(size_t)page * P.Hkv] : 0.0f;
+    const float old = there && off > 0 ? scale[(size_t)page * P.Hkv] : 0.0f;
     float most = old;
 #pragma unroll
-    for (int j = 0; j < MAXV; ++j) most = fmaxf(most, now_s[j]);
+    for (int j = 0; j < MAXV; ++j) most = fmaxf(most, B.s[j]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    float* red = s_red[b & 1];
-    if (lane == 0) red[warp] = most;
-    __syncthreads();                            // (all of this block's sources have been read)
-    most = red[lane & 7];
+    if (UW > 1) {                                 // (all of this block's sources have been read behind it)
+      float* red = s_red[b & 1];
+      if (lane == 0) red[warp] = most;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "n"(TPU) : "memory");
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      for (int i = 0; i < UW; ++i) most = fmaxf(most, red[mine * UW + i]);
+    } else {
+      __syncwarp();
+    }
+    if (!there) return;
     uint8_t* to = codes + (size_t)page * page_codes;
     if (off > 0 && old != most) {
       const float ratio = old / most;
-      for (int i = tid; i < off * vec_tok; i += kCompactThreads) {
+      for (int i = me; i < off << lv; i += TPU) {
         uint4 w = *reinterpret_cast<uint4*>(to + ((size_t)i << 4));
         w.x = e4m3x4_rescale(w.x, ratio); w.y = e4m3x4_rescale(w.y, ratio);
         w.z = e4m3x4_rescale(w.z, ratio); w.w = e4m3x4_rescale(w.w, ratio);
@@ -586,21 +599,32 @@ __global__ void __launch_bounds__(kCompactThreads) k_pages_compact(const Compact
     }
 #pragma unroll
     for (int j = 0; j < MAXV; ++j) {
-      const int x = tid + j * kCompactThreads;
-      if (x < cnt * vec_tok) {
-        uint4 w = now[j];
-        if (now_s[j] != most) {
-          const float ratio = now_s[j] / most;
+      const int x = me + j * TPU;
+      if (x < cnt << lv) {
+        uint4 w = B.w[j];
+        if (B.s[j] != most) {
+          const float ratio = B.s[j] / most;
           w.x = e4m3x4_rescale(w.x, ratio); w.y = e4m3x4_rescale(w.y, ratio);
           w.z = e4m3x4_rescale(w.z, ratio); w.w = e4m3x4_rescale(w.w, ratio);
         }
         *reinterpret_cast<uint4*>(to + (size_t)off * hd + ((size_t)x << 4)) = w;
       }
     }
-    if (tid == 0) scale[(size_t)page * P.Hkv] = most;
-    i0 = ni0; cnt = ncnt; off = noff;
-#pragma unroll
-    for (int j = 0; j < MAXV; ++j) { now[j] = next[j]; now_s[j] = next_s[j]; }
+    if (me == 0) scale[(size_t)page * P.Hkv] = most;
+  };
+  Block A0, A1, A2;
+  ask(A0);
+  ask(A1);
+#pragma unroll 1
+  for (int b = b0; b <= b1; b += 3) {
+    ask(A2);
+    settle(b, A0);
+    if (b + 1 > b1) break;
+    ask(A0);
+    settle(b + 1, A1);
+    if (b + 2 > b1) break;
+    ask(A1);
+    settle(b + 2, A2);
   }
 }
 

@@ -66,14 +66,16 @@ size_t attn_bytes(const tabed_pages* p) {
 }
 
 // As a programmatic dependent of the kernel before it in the stream: every kernel here waits before it touches memory.
+// early = false: when that kernel has ended (the joins: as dependents they slow the next attention's launch down, 96 sequences
+// of 256 - 4096 tokens back to back 103 us, 71 so).
 template <typename ArgT>
-int launch(const tabed_pages* p, void (*kern)(ArgT), dim3 grid, int block, size_t smem, const ArgT& args) {
+int launch(const tabed_pages* p, void (*kern)(ArgT), dim3 grid, int block, size_t smem, const ArgT& args, bool early = true) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = reinterpret_cast<cudaStream_t>(p->stream);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
+  cfg.attrs = at; cfg.numAttrs = early ? 1 : 0;
   if (cudaLaunchKernelEx(&cfg, kern, args) != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
   return TABED_OK;
 }
@@ -110,6 +112,8 @@ int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, int item
   return items <= 512 ? launch_append_long<T, 512, 1>(p, a, grid, smem) : launch_append_long<T, 512, 2>(p, a, grid, smem);
 }
 
+constexpr int kJoinFew = 2, kJoinMany = 4;      // rows of a join's block
+
 template <int HD, bool TWO, bool R8>
 int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
   auto kern = k_pages_attn<HD, TWO, R8>;
@@ -125,7 +129,7 @@ int launch_attn(const tabed_pages* p, const PagesAttnArgs& a) {
   }
   const int ctas = std::min(kPgaMaxCtas, per_sm[p->device] * sm_count(p->device));
   const int rc = launch(p, kern, dim3(ctas), kPgaThreads, pga_smem<HD, R8>(), a);
-  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO>, dim3(ctas, (a.RB + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, TWO, kJoinFew>, dim3(ctas, (a.RB + kJoinFew - 1) / kJoinFew), kJoinThreads, 0, a, false);
 }
 
 template <int HD, int MT, int COPIES>
@@ -138,7 +142,7 @@ int launch_attn_tc(const tabed_pages* p, const PagesAttnArgs& a) {
   }
   const int ctas = std::min(kPtMaxCtas, sm_count(p->device));
   const int rc = launch(p, kern, dim3(ctas), Pt<HD, MT>::kThreads, kPtSmem, a);
-  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, false>, dim3(ctas, (a.RB + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, a);
+  return rc != TABED_OK ? rc : launch(p, k_pages_attn_join<HD, false, kJoinMany>, dim3(ctas, (a.RB + kJoinMany - 1) / kJoinMany), kJoinThreads, 0, a, false);
 }
 
 template <int HD>

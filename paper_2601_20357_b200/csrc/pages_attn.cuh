@@ -609,19 +609,19 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   }
 }
 
-// Puts the parts of the items that span CTAs together: block (c, y) takes four rows of the item that begins in CTA c and goes on behind
+// Puts the parts of the items that span CTAs together: block (c, y) takes ROWS rows of the item that begins in CTA c and goes on behind
 // it.  The weights of all parts come first (their loads are independent), then the parts' outputs, split over the threads that the rows leave.
-constexpr int kJoinRows = 4, kJoinThreads = 256;
+constexpr int kJoinThreads = 256;
 
-template <int HD, bool TWO>
+template <int HD, bool TWO, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) k_pages_attn_join(const PagesAttnArgs A) {
-  constexpr int ITEMS = kJoinRows * HD / 4, SPLIT = kJoinThreads / ITEMS, PER_ROW = kJoinThreads / kJoinRows;
-  __shared__ float s_f[kJoinRows][kPgaMaxCtas + 1], s_red[kJoinRows][2][PER_ROW / 32], s_sum[kJoinRows];
+  constexpr int ITEMS = ROWS * HD / 4, SPLIT = kJoinThreads / ITEMS, PER_ROW = kJoinThreads / ROWS;
+  __shared__ float s_f[ROWS][kPgaMaxCtas + 1], s_red[ROWS][2][PER_ROW / 32], s_sum[ROWS];
   __shared__ float4 s_v[SPLIT > 1 ? SPLIT - 1 : 1][ITEMS];
   __shared__ int s_n;
-  const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, grp = A.H / A.P.Hkv, RB = A.RB, r0 = blockIdx.y * kJoinRows;
-  pdl_trigger();
+  const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, grp = A.H / A.P.Hkv, RB = A.RB, r0 = blockIdx.y * ROWS;
   pdl_wait();
+  pdl_trigger();
   const int4 d = A.desc[c * 2 + 1];
   if (!(d.x & 1)) return;
   const int e = d.y, kvh = d.z, rt = d.w;
@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_pages_attn_join(const PagesAtt
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_red[r][1][w] = sum;
     __syncthreads();
-    if (tid < kJoinRows) {
+    if (tid < ROWS) {
       float x = 0.0f;
 #pragma unroll
       for (int i = 0; i < PER_ROW / 32; ++i) x += s_red[tid][1][i];

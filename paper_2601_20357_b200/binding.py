@@ -38,7 +38,7 @@ EXPORTS = [
     "tabed_last_device_error", "tabed_sync_lengths", "tabed_debug_barrier_timeout", "tabed_static_last_error",
     "tabed_set_policy_uniforms",
     "tabed_pages_workspace", "tabed_pages_fork", "tabed_pages_append", "tabed_pages_attention", "tabed_pages_compact",
-    "tabed_pages_last_error",
+    "tabed_pages_last_error", "tabed_pages_store_row", "tabed_pages_load_row",
 ]
 
 
@@ -141,6 +141,8 @@ def lib() -> C.CDLL:
         L.tabed_pages_attention.argtypes = [pages, C.POINTER(TabedPagesQuery)]
         L.tabed_pages_compact.argtypes = [pages, vp, vp, vp, vp, i32, i32]
         L.tabed_pages_last_error.argtypes = [pages]
+        L.tabed_pages_store_row.argtypes = [vp, pages, i32, i32, i32, i32]
+        L.tabed_pages_load_row.argtypes = [vp, pages, i32, i32, i32]
         L.tabed_launch_count.argtypes = [vp]
         L.tabed_launch_count.restype = C.c_int64
         for name in EXPORTS:
@@ -251,6 +253,14 @@ class Tabed:
         d = tokens.shape[1]
         _check(lib().tabed_pool_embeds(self._h, _ptr(tokens, torch.float32, grid_h * grid_w * d, "tokens", self.device), grid_h, grid_w, d,
                                        _ptr(out, torch.float32, (grid_h // 2) * (grid_w // 2) * d, "out", self.device)), "tabed_pool_embeds")
+
+    def pages_store_row(self, pages: "Pages", row: int, seq: int, start: int, length: int) -> None:
+        """Positions start .. start + length - 1 of a row's committed cache to those of a sequence."""
+        _check(lib().tabed_pages_store_row(self._h, pages._handle, row, seq, start, length), "tabed_pages_store_row")
+
+    def pages_load_row(self, pages: "Pages", row: int, seq: int, length: int) -> None:
+        """The first `length` tokens of a sequence become the row's committed cache."""
+        _check(lib().tabed_pages_load_row(self._h, pages._handle, row, seq, length), "tabed_pages_load_row")
 
     def set_pending(self, tok: torch.Tensor, cnt: torch.Tensor) -> None:
         _check(lib().tabed_set_pending(self._h, _ptr(tok, torch.int32, self.B * 2, "tok", self.device),
@@ -442,7 +452,7 @@ class Pages:
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.ref, self.err, self.workspace = k, v, k_scale, v_scale, table, ref, err, workspace
         self._stream = stream
         self._p = p
-        self._ref = C.byref(p)
+        self._handle = C.byref(p)
 
     def _entries(self, seq: Optional[torch.Tensor], first: torch.Tensor) -> int:
         n = first.numel() - 1
@@ -454,7 +464,7 @@ class Pages:
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, keep: torch.Tensor, length: torch.Tensor) -> None:
         n, d, i = src.numel(), self.device, torch.int32
-        _check(lib().tabed_pages_fork(self._ref, _ptr(src, i, n, "src", d), _ptr(dst, i, n, "dst", d), _ptr(keep, i, n, "keep", d),
+        _check(lib().tabed_pages_fork(self._handle, _ptr(src, i, n, "src", d), _ptr(dst, i, n, "dst", d), _ptr(keep, i, n, "keep", d),
                                       _ptr(length, i, n, "length", d), n), "tabed_pages_fork")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seq: Optional[torch.Tensor], first: torch.Tensor, start: torch.Tensor,
@@ -486,7 +496,7 @@ class Pages:
             t.n_heads = H
             t.q, t.q_stride = _rows(q, k.dtype, T, H, self.hd, "q", d)
             t.q_out, t.q_out_stride = _rows(q_out, k.dtype, T, H, self.hd, "q_out", d)
-        _check(lib().tabed_pages_append(self._ref, C.byref(t)), "tabed_pages_append")
+        _check(lib().tabed_pages_append(self._handle, C.byref(t)), "tabed_pages_append")
 
     def attention(self, layer: int, q: torch.Tensor, out: torch.Tensor, seq: Optional[torch.Tensor], first: torch.Tensor, length: torch.Tensor,
                   max_new: int, *, scale: float, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
@@ -505,19 +515,19 @@ class Pages:
         t.slopes, t.prefix = _ptr(slopes, torch.float32, H, "slopes", d), _ptr(prefix, i, n, "prefix", d)
         if tree is not None:
             t.tree = _ptr(tree, tree.dtype if tree.dtype in (torch.int64, torch.uint64) else torch.int64, T, "tree", d)
-        _check(lib().tabed_pages_attention(self._ref, C.byref(t)), "tabed_pages_attention")
+        _check(lib().tabed_pages_attention(self._handle, C.byref(t)), "tabed_pages_attention")
 
     def compact(self, seq: torch.Tensor, start: torch.Tensor, count: torch.Tensor, index: torch.Tensor) -> None:
         """index [entries][width]"""
         n, d, i = seq.numel(), self.device, torch.int32
         if index.dim() != 2 or index.shape[0] != n:
             raise ValueError("index: expected [entries][width]")
-        _check(lib().tabed_pages_compact(self._ref, _ptr(seq, i, n, "seq", d), _ptr(start, i, n, "start", d), _ptr(count, i, n, "count", d),
+        _check(lib().tabed_pages_compact(self._handle, _ptr(seq, i, n, "seq", d), _ptr(start, i, n, "start", d), _ptr(count, i, n, "count", d),
                                          _ptr(index, i, index.numel(), "index", d), n, index.shape[1]), "tabed_pages_compact")
 
     def last_error(self) -> int:
         """Code of what the calls recorded on the device since the last time (0 if nothing); clears the record."""
-        return int(lib().tabed_pages_last_error(self._ref))
+        return int(lib().tabed_pages_last_error(self._handle))
 
 
 def weights_to_device(drafter, weights_np: Dict[str, object], device: torch.device) -> Dict[str, object]:

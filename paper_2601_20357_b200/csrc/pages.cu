@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "../../include/tabed.h"
+#include "pages.h"
 #include "pages_attn.cuh"
 #include "pages_attn_tc.cuh"
 #include "pages_kernels.cuh"
@@ -112,6 +113,26 @@ int launch_append(const tabed_pages* p, const AppendArgs& a, dim3 grid, int item
   return items <= 512 ? launch_append_long<T, 512, 1>(p, a, grid, smem) : launch_append_long<T, 512, 2>(p, a, grid, smem);
 }
 
+// the launch of an append whose arguments are in place but for its geometry
+int run_append(const tabed_pages* p, AppendArgs& a, bool f32) {
+  const int ps = p->page_tokens, most = std::min(a.max_new, ps);      // tokens of a block
+  a.nblk = (a.max_new + ps - 2) / ps + 1;
+  // Units of a warp where a head's tokens of a block are one item a lane (a token of 128 values has 8 of them)
+  const int items = most * (p->head_dim / 16);
+  const bool small = items <= 32;
+  const int heads = 2 * p->n_kv_heads + (a.has_q ? a.n_heads : 0);
+  const long long blocks = (long long)a.n * a.nblk;
+  if (blocks > 0x7FFFFFFFll) return TABED_ERR_UNSUPPORTED;
+  // heads of a CTA: the cosines serve all of them, as long as the grid keeps some CTAs for every SM
+  const int per = small ? kAppendThreads / 32 : 1;
+  int groups = (int)std::min<long long>((heads + per - 1) / per, std::max<long long>(1, (8ll * sm_count(p->device) + blocks - 1) / blocks));
+  a.hpc = ((heads + groups - 1) / groups + per - 1) / per * per;
+  groups = (heads + a.hpc - 1) / a.hpc;
+  const size_t smem = a.n_axes > 0 ? (size_t)items * 4 * sizeof(float4) : 0;
+  const dim3 grid((unsigned)blocks, (unsigned)groups);
+  return f32 ? launch_append<float>(p, a, grid, items, smem) : launch_append<__nv_bfloat16>(p, a, grid, items, smem);
+}
+
 constexpr int kJoinFew = 2, kJoinMany = 4;      // rows of a join's block
 
 template <int HD, bool TWO, bool R8>
@@ -155,6 +176,45 @@ int launch_attn_hd(const tabed_pages* p, const PagesAttnArgs& a, bool f32) {
 
 }  // namespace
 
+namespace tabed {
+
+int pages_match(const tabed_pages* p, int L, int Hkv, int hd, int device) {
+  const int rc = check(p);
+  if (rc != TABED_OK) return rc;
+  return p->n_layers == L && p->n_kv_heads == Hkv && p->head_dim == hd && p->device == device ? TABED_OK : TABED_ERR_INVALID_ARG;
+}
+
+int pages_store_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r, int seq, int start, int len, int64_t* launches) {
+  tabed_pages here = *p;
+  here.stream = stream;
+  const int hd = p->head_dim;
+  const size_t esz = r.f32 ? 4 : 2;
+  AppendArgs a = {};
+  a.P = on_device(p); a.n = 1; a.n_tokens = len; a.max_new = len; a.seq0 = seq; a.start0 = start;
+  a.kv_stride = hd; a.kv_head = (long long)r.cap * hd; a.vec_kv = 1;
+  for (a.layer = 0; a.layer < p->n_layers; ++a.layer) {
+    const size_t at = ((size_t)a.layer * p->n_kv_heads * r.cap + start) * hd * esz;
+    a.k = static_cast<const char*>(r.k) + at; a.v = static_cast<const char*>(r.v) + at;
+    const int rc = run_append(&here, a, r.f32);
+    if (rc != TABED_OK) return rc;
+    ++*launches;
+  }
+  return TABED_OK;
+}
+
+int pages_load_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r, int seq, int len, int* kv_len, int64_t* launches) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((len + p->page_tokens - 1) / p->page_tokens, 2 * p->n_kv_heads, p->n_layers); cfg.blockDim = dim3(128); cfg.stream = stream;
+  const PagesDev d = on_device(p);
+  const cudaError_t rc = r.f32 ? cudaLaunchKernelEx(&cfg, k_pages_load_row<float>, d, seq, len, static_cast<float*>(r.k), static_cast<float*>(r.v), r.cap, kv_len)
+                               : cudaLaunchKernelEx(&cfg, k_pages_load_row<__nv_bfloat16>, d, seq, len, static_cast<__nv_bfloat16*>(r.k), static_cast<__nv_bfloat16*>(r.v), r.cap, kv_len);
+  if (rc != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
+  ++*launches;
+  return TABED_OK;
+}
+
+}  // namespace tabed
+
 extern "C" {
 
 int tabed_pages_workspace(const tabed_pages* p, size_t* bytes) {
@@ -180,8 +240,13 @@ int tabed_pages_fork(const tabed_pages* p, const int32_t* src, const int32_t* ds
   a.rows = reinterpret_cast<int*>(ws); ws += round16((size_t)p->n_seqs * p->max_pages * 4);
   a.free_list = reinterpret_cast<int*>(ws);
   a.vec_ref = aligned(p->ref, 16);
-  int rc = launch(p, k_pages_share, dim3(n), kForkThreads, 0, a);
-  if (rc == TABED_OK) rc = launch(p, k_pages_alloc, dim3(1), kForkAllocThreads, 0, a);
+  int rc;
+  if (n <= kPlanEntries && (long long)n * p->max_pages <= kPlanBlocks) {      // (3 entries of 13 blocks 10.3 -> 9.3 us; 96 of 67 would go from 11.9 to 17.4)
+    rc = launch(p, k_pages_plan, dim3(1), kForkAllocThreads, 0, a);
+  } else {
+    rc = launch(p, k_pages_share, dim3(n), kForkThreads, 0, a);
+    if (rc == TABED_OK) rc = launch(p, k_pages_alloc, dim3(1), kForkAllocThreads, 0, a);
+  }
   if (rc == TABED_OK) rc = launch(p, k_pages_settle, dim3(n, 1 + 2 * p->n_layers), kForkThreads, 0, a);
   return rc;
 }
@@ -217,28 +282,13 @@ int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t) {
   AppendArgs a = {};
   a.P = on_device(p); a.layer = t->layer; a.n = t->n; a.n_tokens = t->n_tokens; a.max_new = t->max_new; a.n_heads = t->n_heads;
   a.seq = t->seq; a.first = t->first; a.start = t->start; a.positions = t->positions; a.k = t->k; a.v = t->v; a.q = t->q; a.q_out = t->q_out;
-  a.kv_stride = t->kv_stride; a.q_stride = t->q_stride; a.q_out_stride = t->q_out_stride; a.n_axes = t->n_axes; a.has_q = with_q;
+  a.kv_stride = t->kv_stride; a.kv_head = hd; a.q_stride = t->q_stride; a.q_out_stride = t->q_out_stride; a.n_axes = t->n_axes; a.has_q = with_q;
   a.vec_kv = rows_aligned(t->k, t->kv_stride, esz) && aligned(t->v, 16);
   a.vec_q = with_q && rows_aligned(t->q, t->q_stride, esz) && rows_aligned(t->q_out, t->q_out_stride, esz);
   for (int i = 0; i < t->n_axes; ++i) a.sections[i] = t->sections[i];
   if (t->n_axes > 0)
     for (int i = 0; i < half; ++i) a.turns[i] = pow((double)t->theta, -2.0 * i / hd) / 6.283185307179586476925;
-  const int ps = p->page_tokens, most = std::min(t->max_new, ps);      // tokens of a block
-  a.nblk = (t->max_new + ps - 2) / ps + 1;
-  // Units of a warp where a head's tokens of a block are one item a lane (a token of 128 values has 8 of them)
-  const int items = most * (hd / 16);
-  const bool small = items <= 32;
-  const int heads = 2 * p->n_kv_heads + (with_q ? t->n_heads : 0);
-  const long long blocks = (long long)t->n * a.nblk;
-  if (blocks > 0x7FFFFFFFll) return TABED_ERR_UNSUPPORTED;
-  // heads of a CTA: the cosines serve all of them, as long as the grid keeps some CTAs for every SM
-  const int per = small ? kAppendThreads / 32 : 1;
-  int groups = (int)std::min<long long>((heads + per - 1) / per, std::max<long long>(1, (8ll * sm_count(p->device) + blocks - 1) / blocks));
-  a.hpc = ((heads + groups - 1) / groups + per - 1) / per * per;
-  groups = (heads + a.hpc - 1) / a.hpc;
-  const size_t smem = t->n_axes > 0 ? (size_t)items * 4 * sizeof(float4) : 0;
-  const dim3 grid((unsigned)blocks, (unsigned)groups);
-  return t->dtype == TABED_DTYPE_FP32 ? launch_append<float>(p, a, grid, items, smem) : launch_append<__nv_bfloat16>(p, a, grid, items, smem);
+  return run_append(p, a, t->dtype == TABED_DTYPE_FP32);
 }
 
 int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {

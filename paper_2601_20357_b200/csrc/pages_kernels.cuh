@@ -60,10 +60,11 @@ __device__ __forceinline__ float least_scale(float amax) {
 struct AppendArgs {
   PagesDev P;
   int layer, n, n_tokens, max_new, n_heads, nblk, hpc, n_axes, has_q;
-  const int *seq, *first, *start, *positions;
+  const int *seq, *first, *start, *positions;      // seq null: entry e is sequence seq0 + e; first null: one entry, all tokens, from start0 on
+  int seq0, start0;
   const void *k, *v, *q;
   void* q_out;
-  long long kv_stride, q_stride, q_out_stride;
+  long long kv_stride, kv_head, q_stride, q_out_stride;      // elements between tokens; between heads of K and V
   int vec_kv, vec_q;                  // rows start on 16-byte boundaries
   int sections[4];
   double turns[64];                   // theta^(-2 i / hd) / (2 pi)
@@ -164,7 +165,8 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
   const int e = blockIdx.x / A.nblk, slot = blockIdx.x - e * A.nblk;
   pdl_trigger();
   pdl_wait();
-  const int s = A.seq ? A.seq[e] : e, f0 = A.first[e], f1 = A.first[e + 1], p0 = A.start[e], ps = P.ps, hd = P.hd, half = hd >> 1;
+  const int s = A.seq ? A.seq[e] : A.seq0 + e, f0 = A.first ? A.first[e] : 0, f1 = A.first ? A.first[e + 1] : A.n_tokens, p0 = A.start ? A.start[e] : A.start0;
+  const int ps = P.ps, hd = P.hd, half = hd >> 1;
   if (f0 < 0 || f1 < f0 || f1 > A.n_tokens || s < 0 || s >= P.n_seqs || p0 < 0 || f1 - f0 > A.max_new) {
     if (tid == 0) atomicOr(P.err, PGERR_INVALID);
     return;
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
   Raw8<T> ra[MAXI], rb[MAXI];
   auto ask = [&](int u) {                         // unit u's values
     const bool is_q = u >= 2 * P.Hkv, is_v = !is_q && u >= P.Hkv;
-    const T* in = reinterpret_cast<const T*>(is_q ? A.q : (is_v ? A.v : A.k)) + (size_t)(is_q ? u - 2 * P.Hkv : (is_v ? u - P.Hkv : u)) * hd;
+    const T* in = reinterpret_cast<const T*>(is_q ? A.q : (is_v ? A.v : A.k)) + (is_q ? (size_t)(u - 2 * P.Hkv) * hd : (size_t)(is_v ? u - P.Hkv : u) * A.kv_head);
     const long long stride = is_q ? A.q_stride : A.kv_stride;
     const bool vec = is_q ? A.vec_q : A.vec_kv;
 #pragma unroll
@@ -306,9 +308,41 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
   }
 }
 
+// The other way: the first `len` tokens of a sequence into a dense cache row [L][Hkv][cap][hd] (a code times a power of two is a bf16 value
+// already).  Blocks without a page become zeros.  grid (ceil(len / page_tokens), 2 Hkv, L)
+template <typename T>
+__global__ void __launch_bounds__(128) k_pages_load_row(const PagesDev P, int seq, int len, T* __restrict__ k, T* __restrict__ v, int cap, int* kv_len) {
+  const int b = blockIdx.x, head = blockIdx.y >> 1, layer = blockIdx.z, hd = P.hd, tid = threadIdx.x;
+  const bool is_v = blockIdx.y & 1;
+  pdl_trigger();
+  pdl_wait();
+  int page = P.table[(size_t)seq * P.max_pages + b];
+  if (page < 0 || page >= P.NP) {
+    if (tid == 0) atomicOr(P.err, PGERR_INVALID);
+    page = -1;
+  }
+  if (tid == 0 && b == 0 && blockIdx.y == 0 && layer == 0) *kv_len = len;
+  const size_t at = ((size_t)layer * P.NP + max(page, 0)) * P.Hkv + head;
+  const uint8_t* codes = (is_v ? P.v : P.k) + at * P.ps * hd;
+  const float scale = page >= 0 ? (is_v ? P.v_scale : P.k_scale)[at] : 0.0f;
+  T* out = (is_v ? v : k) + (((size_t)layer * P.Hkv + head) * cap + (size_t)b * P.ps) * hd;
+  const int n = min(P.ps, len - b * P.ps) * hd;
+  for (int i = tid * 8; i < n; i += 128 * 8) {
+    const uint2 c = page >= 0 ? *reinterpret_cast<const uint2*>(codes + i) : make_uint2(0u, 0u);
+    uint32_t h[4];
+    e4m3x4_to_f16x4(c.x, h[0], h[1]);
+    e4m3x4_to_f16x4(c.y, h[2], h[3]);
+    float f[8];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) { const float2 y = f16x2_to_float2(h[x]); f[2 * x] = y.x * scale; f[2 * x + 1] = y.y * scale; }
+    store8(out + i, true, f);
+  }
+}
+
 // ---- fork ------------------------------------------------------------------------------------------
 // Three launches: the references of the pages shared, pinned and given back (a CTA an entry; atomic additions, whose order does
-// not matter), the free pages (one CTA: who needs how many, and the lowest-numbered ones in order), the tables and the copies.
+// not matter), the free pages (one CTA: who needs how many, and the lowest-numbered ones in order), the tables and the copies.  The
+// first two are one CTA's launch for few and short tables.
 // While the call runs a page's word in `ref` holds its references in the low half and in the high half how many entries copy from
 // it: such a page is not handed out even where nobody names it any longer.
 struct ForkEntry { int valid, stays, first_new, tail; };     // tail: page of the block that keep ends in, -1 if it ends with a block
@@ -382,19 +416,17 @@ __device__ __forceinline__ int block_scan(int v, int* s_scan, int* total) {
   return before;
 }
 
-__global__ void __launch_bounds__(kForkAllocThreads) k_pages_alloc(const ForkArgs A) {
-  __shared__ int s_scan[33];
+// Who needs how many pages, and the free ones in order: one CTA.
+__device__ __forceinline__ void fork_alloc(const ForkArgs& A, int* s_scan) {
   const PagesDev& P = A.P;
   const int tid = threadIdx.x;
-  pdl_trigger();
-  pdl_wait();
   int need_all = 0;
   for (int base = 0; base < A.n; base += kForkAllocThreads) {
     const int e = base + tid;
     int need = 0;
     if (e < A.n && A.ent[e].valid) {
       const int keep = A.keep[e], full = keep / P.ps, tail = A.ent[e].tail;
-      const int stays = tail >= 0 && A.src[e] == A.dst[e] && (P.ref[tail] & 0xFFFF) == 0;
+      const int stays = tail >= 0 && A.src[e] == A.dst[e] && (__ldcg(P.ref + tail) & 0xFFFF) == 0;
       need = (A.len[e] + P.ps - 1) / P.ps - full - stays;
       A.ent[e].stays = stays;
     }
@@ -414,10 +446,10 @@ __global__ void __launch_bounds__(kForkAllocThreads) k_pages_alloc(const ForkArg
     int r[PER], mine = 0;
     if (A.vec_ref && p0 + PER <= P.NP) {
 #pragma unroll
-      for (int j = 0; j < PER; j += 4) *reinterpret_cast<int4*>(r + j) = *reinterpret_cast<const int4*>(P.ref + p0 + j);
+      for (int j = 0; j < PER; j += 4) *reinterpret_cast<int4*>(r + j) = __ldcg(reinterpret_cast<const int4*>(P.ref + p0 + j));
     } else {
 #pragma unroll
-      for (int j = 0; j < PER; ++j) r[j] = p0 + j < P.NP ? P.ref[p0 + j] : 1;
+      for (int j = 0; j < PER; ++j) r[j] = p0 + j < P.NP ? __ldcg(P.ref + p0 + j) : 1;
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j) mine += r[j] == 0;
@@ -431,6 +463,63 @@ __global__ void __launch_bounds__(kForkAllocThreads) k_pages_alloc(const ForkArg
     A.found[0] = min(found, need_all);
     if (found < need_all) atomicOr(P.err, PERR_KV);
   }
+}
+
+__global__ void __launch_bounds__(kForkAllocThreads) k_pages_alloc(const ForkArgs A) {
+  __shared__ int s_scan[33];
+  pdl_trigger();
+  pdl_wait();
+  fork_alloc(A, s_scan);
+}
+
+// k_pages_share and k_pages_alloc in one launch of one CTA, for few and short tables (the threads go over all entries' blocks together).
+constexpr int kPlanEntries = kForkAllocThreads, kPlanBlocks = 1024;
+__global__ void __launch_bounds__(kForkAllocThreads) k_pages_plan(const ForkArgs A) {
+  __shared__ int s_scan[33], s_src[kPlanEntries], s_dst[kPlanEntries], s_keep[kPlanEntries], s_bad[kPlanEntries];
+  const PagesDev& P = A.P;
+  const int tid = threadIdx.x, W = P.max_pages;
+  pdl_trigger();
+  pdl_wait();
+  bool over = false;
+  if (tid < A.n) {
+    const int src = A.src[tid], dst = A.dst[tid], keep = A.keep[tid], len = A.len[tid];
+    bool bad = src < 0 || src >= P.n_seqs || dst < 0 || dst >= P.n_seqs || keep < 0 || len < keep;
+    over = !bad && len > W * P.ps;
+    bad |= over;
+    s_src[tid] = bad ? 0 : src; s_keep[tid] = bad ? 0 : keep; s_dst[tid] = dst; s_bad[tid] = bad;
+  }
+  __syncthreads();
+  if (tid < A.n) {
+    const int dst = s_dst[tid];
+    bool twice = false;
+    for (int i = 0; i < A.n; ++i) twice |= i != tid && s_dst[i] == dst;
+    if (twice) s_bad[tid] = 1;
+  }
+  for (int i = tid; i < A.n * W; i += kForkAllocThreads) {
+    const int e = i / W, b = i - e * W;
+    if (b < (s_keep[e] + P.ps - 1) >> P.ls) { const int pg = P.table[(size_t)s_src[e] * W + b]; if (pg < 0 || pg >= P.NP) s_bad[e] = 1; }
+  }
+  __syncthreads();
+  if (tid < A.n) {
+    const bool bad = s_bad[tid];
+    const int keep = s_keep[tid], tail = bad || (keep & (P.ps - 1)) == 0 ? -1 : P.table[(size_t)s_src[tid] * W + (keep >> P.ls)];
+    A.ent[tid] = ForkEntry{!bad, 0, 0, tail};
+    if (bad) atomicOr(P.err, over ? PERR_KV : PGERR_INVALID);
+    if (tail >= 0) atomicAdd(P.ref + tail, 1 << 16);
+  }
+  for (int i = tid; i < A.n * W; i += kForkAllocThreads) {
+    const int e = i / W, b = i - e * W;
+    if (s_bad[e]) continue;
+    if (b < s_keep[e] >> P.ls) {
+      const int pg = P.table[(size_t)s_src[e] * W + b];
+      A.rows[(size_t)e * W + b] = pg;
+      atomicAdd(P.ref + pg, 1);
+    }
+    const int pg = P.table[(size_t)s_dst[e] * W + b];
+    if (pg >= 0 && pg < P.NP) atomicAdd(P.ref + pg, -1);
+  }
+  __syncthreads();
+  fork_alloc(A, s_scan);
 }
 
 // grid (n, 1 + 2 L): the table, then K and V of a layer

@@ -23,6 +23,7 @@
 #include "attn_tc.cuh"
 #include "prompt_attn.cuh"
 #include "request_kernels.cuh"
+#include "pages.h"
 
 using namespace tabed;
 
@@ -1158,6 +1159,36 @@ int tabed_load_prefix_kv(tabed_handle* h, int32_t row, const void* k, const void
     return TABED_ERR_CUDA;
   h->len_ub[row] = len;
   return TABED_OK;
+}
+
+static DenseRow dense_row(tabed_handle* h, int row) {
+  const size_t bytes = (size_t)h->L * h->Hkv * h->cap * h->hd * h->esz;
+  return DenseRow{static_cast<unsigned char*>(h->kc) + row * bytes, static_cast<unsigned char*>(h->vc) + row * bytes, h->cap, h->esz == 4};
+}
+
+int tabed_pages_store_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t start, int32_t len) {
+  if (!h || !p) return TABED_ERR_NULL_PTR;
+  if (!h->has_drafter || h->phase != PH_IDLE) return TABED_ERR_BAD_STATE;
+  const int rc = pages_match(p, h->L, h->Hkv, h->hd, h->cfg.device);
+  if (rc != TABED_OK) return rc;
+  if (row < 0 || row >= h->R || seq < 0 || seq >= p->n_seqs || start < 0 || len < 1 || len > h->len_ub[row] || start > h->len_ub[row] - len) return TABED_ERR_INVALID_ARG;
+  if ((long long)start + len > (long long)p->max_pages * p->page_tokens) return TABED_ERR_KV_OVERFLOW;
+  DeviceGuard guard(h->cfg.device);
+  return guard.ok ? pages_store_row(p, h->stream, dense_row(h, row), seq, start, len, &h->launches) : TABED_ERR_CUDA;
+}
+
+int tabed_pages_load_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t len) {
+  if (!h || !p) return TABED_ERR_NULL_PTR;
+  if (!h->has_drafter || h->phase != PH_IDLE) return TABED_ERR_BAD_STATE;
+  int rc = pages_match(p, h->L, h->Hkv, h->hd, h->cfg.device);
+  if (rc != TABED_OK) return rc;
+  if (row < 0 || row >= h->R || seq < 0 || seq >= p->n_seqs || len < 1 || len > h->cap) return TABED_ERR_INVALID_ARG;
+  if (len > (long long)p->max_pages * p->page_tokens) return TABED_ERR_KV_OVERFLOW;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return TABED_ERR_CUDA;
+  rc = pages_load_row(p, h->stream, dense_row(h, row), seq, len, h->kv_len + row, &h->launches);
+  if (rc == TABED_OK) h->len_ub[row] = len;
+  return rc;
 }
 
 static int prefill_common(tabed_handle* h, int32_t row, const int32_t* tokens, const float* embeds, int32_t len) {

@@ -579,6 +579,72 @@ def test_a_request_from_its_prompt_to_its_verified_tree():
     assert not p.ref.any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,d,ps", [(4, 2, 256, 16), (4, 4, 128, 64), (2, 1, 256, 32)])
+def test_rows_of_a_handle_are_parked_in_pages_and_filled_from_them(heads, kv_heads, d, ps, dtype):
+    """A row goes to pages to the bit as the definition has it; two rows filled from a fork of it give the logits, to the bit, of
+    rows that were given the same values by tabed_load_prefix_kv."""
+    import gpu_harness as H
+    from paper_2601_20357_b200 import workloads as W
+    hd, L, n, cap = d // heads, 2, 75, 120
+    wl = W.Workload(name="pages", config_id=95, drafter=W.DrafterCfg(L, d, heads, kv_heads, 256, 1000, dtype), n_inputs=3, n_requests=1, gamma=2, window_h=4,
+                    rounds=1, policy=W.POLICY_STATIC, kv_capacity=cap)
+    w = TB.weights_to_device(wl.drafter, W.make_weights(wl), DEV)
+    c = make([], L=L, Hkv=kv_heads, ps=ps, hd=hd, spare=40, blocks=8, seqs=3)
+    p = to_gpu(c)
+    g, plain = H.make_gpu(wl, w), H.make_gpu(wl, w)
+    r = np.random.default_rng(4)
+    k, v = (torch.from_numpy(r.standard_normal((L, kv_heads, n, hd)) * 0.5).to(DEV, TYPES[dtype]).contiguous() for _ in range(2))
+    for row in range(3):
+        g.load_prefix_kv(row, k, v)
+    forked(c, p, [0], [0], [0], [n])
+    g.pages_store_row(p, 1, 0, 0, 40)
+    g.pages_store_row(p, 2, 0, 40, n - 40)                  # (in two pieces: the second joins the first one's block)
+    for layer in range(L):
+        x = [t[layer].transpose(0, 1).double().cpu().numpy() for t in (k, v)]
+        O.append(c, layer, x[0][:40], x[1][:40], [0], [0, 40], [0])
+        O.append(c, layer, x[0][40:], x[1][40:], [0], [0, n - 40], [40])
+    got = from_gpu(p)
+    for name in ("k", "v"):
+        if n % ps:
+            for t in (got, c):
+                t[name][:, c["table"][0, n // ps], :, n % ps:] = 0
+    same(got, c)
+    p.fork(ints([0]), ints([1]), ints([61]), ints([61]))
+    for row, (seq, m) in enumerate([(0, n), (1, 61), (1, 33)]):
+        g.pages_load_row(p, row, seq, m)
+        dense = [torch.from_numpy(np.stack([O.gather(c, layer, 0, m, x) for layer in range(L)])).to(DEV, TYPES[dtype]).contiguous() for x in "kv"]
+        plain.load_prefix_kv(row, *dense)
+    assert g.debug_view(TB.VIEW_KV_LEN).tolist() == [n, 61, 33] and p.last_error() == 0
+    for _ in range(3):
+        tok = ints([17])
+        a, b = torch.empty((3, 1000), device=DEV), torch.zeros((3, 1000), device=DEV)
+        g.decode_step(tok, a)
+        plain.decode_step(tok, b)
+        assert torch.equal(a, b)
+    # what they refuse
+    other = to_gpu(make([], L=L + 1, Hkv=kv_heads, ps=ps, hd=hd, spare=4, blocks=8, seqs=3))
+    for args, code in [((other, 0, 0, 0, 5), -1), ((p, 3, 0, 0, 5), -1), ((p, -1, 0, 0, 5), -1), ((p, 0, 3, 0, 5), -1), ((p, 0, 0, -1, 5), -1), ((p, 0, 0, 0, 0), -1),
+                       ((p, 0, 0, 0, n + 4), -1), ((p, 0, 0, 2 ** 31 - 1, 5), -1)]:
+        with pytest.raises(TB.TabedError) as e:
+            g.pages_store_row(*args)
+        assert e.value.code == code, args[1:]
+    for args, code in [((other, 0, 0, 5), -1), ((p, 3, 0, 5), -1), ((p, 0, -1, 5), -1), ((p, 0, 0, 0), -1), ((p, 0, 0, cap + 1), -1)]:
+        with pytest.raises(TB.TabedError) as e:
+            g.pages_load_row(*args)
+        assert e.value.code == code, args[1:]
+    g.pages_load_row(p, 0, 2, 20)                           # a sequence without pages: zeros, and a word about it
+    assert p.last_error() == TB.ERR_INVALID_ARG
+    assert p.last_error() == 0
+    for h in (g, plain):
+        h.destroy()
+    empty = TB.Tabed(n_inputs=2, n_requests=1, gamma=1, window_h=1, policy=TB.POLICY_STATIC, vocab=100)
+    with pytest.raises(TB.TabedError) as e:
+        empty.pages_load_row(p, 0, 0, 5)
+    assert e.value.code == TB.ERR_BAD_STATE
+    empty.destroy()
+
+
 def test_steps_captured_in_graphs_that_share_a_workspace():
     """append + attention of two caches on one stream, captured one graph each over one workspace, replayed in turn: what the
     calls give eagerly.  And a call on a stream of its own waits for nothing else."""

@@ -65,6 +65,7 @@ def test_null_pointers():
     L, p = B.lib(), C.byref(pages())
     n = C.c_size_t()
     assert L.tabed_pages_workspace(None, C.byref(n)) == -2 and L.tabed_pages_workspace(p, None) == -2 and L.tabed_pages_last_error(None) == -2
+    assert L.tabed_pages_store_row(None, p, 0, 0, 0, 1) == -2 and L.tabed_pages_load_row(None, p, 0, 0, 1) == -2
     for i in range(4):
         a = [ADDR] * 4
         a[i] = None

@@ -8,8 +8,8 @@
 //   MT = 2 tiles of 128 rows share the converted K and V, and one's softmax runs under the other's products; with MT = 1 two threads have a
 //   row, half of a chunk's positions each, and the scores of the next chunk are computed meanwhile.  Items of up to 64 rows have them twice in
 //   the tile, and a copy takes half of the positions: the products cost the same, the softmax a half; the copies are put together at the end.
-// * Four warps load codes straight into registers, a chunk ahead (a thread has one position; through a ring in shared memory the codes would
-//   cost its bandwidth twice more, which binds), turn them into fp16 and store K and V alike as [dims / 8][128 positions][8 dims]: that is
+// * Eight warps load codes straight into registers, a chunk ahead (through a ring in shared memory the codes would cost its bandwidth
+//   twice more), turn them into fp16 and store K and V alike as [dims / 8][128 positions][8 dims]: that is
 //   K's K-major layout and V's MN-major one.  Half of the codes go through the conversion unit (16 a clock and SM, which the
 //   exponentials need too), half are shifted into place, which leaves them 2^8 too small: undone in q and in the output.
 // * One warp walks the list, looks pages and scales up and tells the others; one issues the products.
@@ -23,7 +23,7 @@ constexpr int kPtChunk = 128;
 constexpr int kPtStart = 2;                    // chunks that an item's beginning and end cost
 constexpr int kPtInfo = 8;                     // chunks that are known ahead
 constexpr int kPtMaxCtas = 160, kPtMaxRows = 256;
-constexpr size_t kPtSmem = 162u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
+constexpr size_t kPtSmem = 200u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
 
 struct PtTile {
   int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, gaps;      // gaps: positions without a page
@@ -32,9 +32,9 @@ struct PtTile {
 };
 
 template <int HD, int MT> struct Pt {
-  static constexpr int kThreads = 32 * 14;                             // 8 warps for the softmax, 4, 1, 1
+  static constexpr int kThreads = 32 * 18;                             // 8 warps each for the softmax and the conversion, 1, 1
   static constexpr int kOp = kPtChunk * HD * 2;                        // fp16 operand of 128 rows or positions
-  static constexpr int kQOff = 0, kKOff = MT * kOp, kVOff = kKOff + kOp, kEnd = kVOff + 2 * kOp;
+  static constexpr int kQOff = 0, kKOff = MT * kOp, kVOff = kKOff + 2 * kOp, kEnd = kVOff + 2 * kOp;
   static_assert(1024 + kEnd <= (int)kPtSmem, "shared memory");
 };
 
@@ -117,10 +117,10 @@ template <int HD, int MT, int COPIES>
 __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const PagesAttnArgs A) {
   using L = Pt<HD, MT>;
   constexpr unsigned FULL = 0xffffffffu;
-  constexpr int W_CONV = 8, W_LOOK = 12, W_MMA = 13;
+  constexpr int W_CONV = 8, W_LOOK = 16, W_MMA = 17;
   extern __shared__ __align__(128) unsigned char pt_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pt_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full, k_empty, v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
+  __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
   __shared__ PtTile info[kPtInfo];
   __shared__ PgaShare s_share;
   __shared__ float s_cr[128 * MT];               // 1 / scale of the query rows
@@ -134,8 +134,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
   constexpr int RP = 128 / COPIES;               // rows of a tile before they repeat
   if (tid == 0) {
     for (int i = 0; i < kPtInfo; ++i) { mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 9); }       // (read by the softmax warps and the products')
-    mbar_init(&k_full, 4); mbar_init(&k_empty, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], MT == 2 ? 4 : 8); mbar_init(&o_done[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&k_full[i], 8); mbar_init(&k_empty[i], 1); mbar_init(&v_full[i], 8); mbar_init(&v_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], MT == 2 ? 4 : 8); mbar_init(&o_done[i], 1); }
     s_dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -216,11 +215,11 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     bool ok = true;
     auto scores = [&](int j, int m) {             // S of chunk j for tile m, into buffer b
       const uint32_t d = tmem + (MT == 2 ? m : (j & 1)) * 128;
-      const uint64_t dq = d_q + (uint64_t)(m * (L::kOp >> 4));
+      const uint64_t dq = d_q + (uint64_t)(m * (L::kOp >> 4)), dk = d_k + (uint64_t)((j & 1) * (L::kOp >> 4));
       if (one) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) pt_mma_ss(d, dq + k * 256, d_k + k * 256, id_s, k > 0);
-        if (m == MT - 1) pt_commit(&k_empty);
+        for (int k = 0; k < HD / 16; ++k) pt_mma_ss(d, dq + k * 256, dk + k * 256, id_s, k > 0);
+        if (m == MT - 1) pt_commit(&k_empty[j & 1]);
         pt_commit(&s_full[MT == 2 ? m : (j & 1)]);
       }
       __syncwarp();
@@ -238,7 +237,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       __syncwarp();
     };
     auto wait = [&](uint64_t* bar, unsigned parity) { if (ok) { ok = pga_wait(bar, parity, dead, P.err); ok = __all_sync(FULL, ok); } };
-    auto k_ready = [&](int j) { wait(&k_full, (unsigned)j & 1u); pt_fence_after(); };
+    auto k_ready = [&](int j) { wait(&k_full[j & 1], (unsigned)(j >> 1) & 1u); pt_fence_after(); };
     const int ahead = MT == 2 ? 1 : 2;            // chunks whose scores are asked for before the first output
     for (int j = 0; j < ahead && j < total && ok; ++j) {
       k_ready(j);
@@ -269,26 +268,26 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     if (!ok) __nanosleep(100000);
   } else if (warp >= W_CONV && warp < W_LOOK) {
     // ---- conversion ----
-    // A warp has 32 positions.  A lane has one 32-byte piece of every (32 / RS)th of them: eight neighbouring lanes have
+    // A warp has 16 positions (one page's).  A lane has one 32-byte piece of every (16 / RS)th of them: eight neighbouring lanes have
     // neighbouring positions (stores free of bank conflicts), and together the lanes read whole rows (few lines a load).
-    const int ct = tid - 32 * W_CONV, cw = ct >> 5;
-    constexpr int NP = HD / 32, RS = 32 / NP;
-    const int piece = lane / RS, row0 = cw * 32 + lane % RS;
+    const int cw = warp - W_CONV;
+    constexpr int NP = HD / 32, RS = NP == 4 ? 8 : 16, NI = 16 / RS;
+    const int piece = lane / RS % NP, row0 = cw * 16 + lane % RS;
+    const bool works = NP > 1 || lane < 16;       // (a row of 32 bytes: 16 lanes)
     const bool vec = A.vec_q;
-    Row32 kr[NP], vr[NP];
-    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NP]) {
-      const uint8_t* base = codes + ((size_t)A.layer * P.NP * Hkv + T.kvh) * (ps * HD) + piece * 32;
+    Row32 kr[NI], vr[NI];
+    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NI]) {
+      const int page = T.page[cw], j = T.j0 + cw * 16;
+      const uint8_t* p = codes + (((size_t)A.layer * P.NP + max(page, 0)) * Hkv + T.kvh) * (ps * HD) + ((j & (ps - 1)) + lane % RS) * HD + piece * 32;
+      const int live = page >= 0 ? T.lim_max - j - lane % RS : 0;      // (what nobody sees becomes zeros: 0 * NaN is not 0)
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int at = row0 + i * RS, page = T.page[at >> 4];
-        const bool there = page >= 0 && T.j0 + at < T.lim_max;      // (what nobody sees becomes zeros: 0 * NaN is not 0)
-        r[i] = ldg32_if(base + (there ? (size_t)page * Hkv * (ps * HD) + (size_t)((T.j0 + at) & (ps - 1)) * HD : 0), there);
-      }
+      for (int i = 0; i < NI; ++i) r[i] = ldg32_if(p + i * RS * HD, works && i * RS < live);
     };
-    auto put = [&](unsigned char* dst, const Row32 (&r)[NP]) {      // 16 codes through the conversion unit, 16 shifted
+    auto put = [&](unsigned char* dst, const Row32 (&r)[NI]) {      // 16 codes through the conversion unit, 16 shifted
       unsigned char* o = dst + piece * 4 * 2048 + row0 * 16;
+      if (!works) return;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
+      for (int i = 0; i < NI; ++i) {
         uint4 a, b, c, d;
         e4m3x4_to_f16x4(r[i].w[0], a.x, a.y); e4m3x4_to_f16x4(r[i].w[1], a.z, a.w);
         e4m3x4_to_f16x4(r[i].w[2], b.x, b.y); e4m3x4_to_f16x4(r[i].w[3], b.z, b.w);
@@ -311,12 +310,14 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     for (int j = 0; j < total; ++j) {
       const PtTile& T = info[j % kPtInfo];
       const PtTile& N = info[(j + 1) % kPtInfo];
-      if (j > 0) { pga_wait(&k_empty, (unsigned)(j - 1) & 1u, dead, P.err); __syncwarp(); }
-      if (T.first) {                              // the item's query rows (all scores of the item before are done): a lane has every fourth 16-byte piece
-        const int nr = T.nq * grp;                // of 8 rows a step, so that four lanes read 64 bytes of a row
+      if (j > 1) { pga_wait(&k_empty[j & 1], (unsigned)((j >> 1) - 1) & 1u, dead, P.err); __syncwarp(); }
+      if (T.first) {                              // the item's query rows (once all scores of the item before are done): a lane has every fourth 16-byte piece of 8 rows a
+                                                  // step, so that four lanes read 64 bytes of a row
+        if (j > 0) { pga_wait(&k_empty[(j - 1) & 1], (unsigned)((j - 1) >> 1) & 1u, dead, P.err); __syncwarp(); }
+        const int nr = T.nq * grp;
 #pragma unroll 1
-        for (int step = 0; step < 4 * MT; ++step) {
-          const int at = (step >> 2) * 128 + cw * 32 + (step & 3) * 8 + (lane & 7), r = (step >> 2) * 128 + (at & 127) % RP, row = T.rt * RB + r;
+        for (int step = 0; step < 2 * MT; ++step) {
+          const int at = (step >> 1) * 128 + cw * 16 + (step & 1) * 8 + (lane & 7), r = (step >> 1) * 128 + (at & 127) % RP, row = T.rt * RB + r;
           const bool there = r < RB && row < nr;
           const int tok = there ? row / grp : 0, h = T.kvh * grp + (there ? row - tok * grp : 0), d0 = (lane >> 3) * 8;
           const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(A.q) + (long long)(T.q0 + tok) * A.q_stride + (long long)h * HD + d0;
@@ -349,13 +350,13 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           // (dims whose codes are shifted: 2^8 more; they are the second 16 of every 32, lanes 16 on)
           const float u = lane >= 16 ? up : up * (1.0f / 256.0f);
           auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * u, __uint_as_float(v & 0xFFFF0000u) * u); };
-          unsigned char* dst = sm + L::kQOff + (step >> 2) * L::kOp + (d0 >> 3) * 2048 + (at & 127) * 16;
+          unsigned char* dst = sm + L::kQOff + (step >> 1) * L::kOp + (d0 >> 3) * 2048 + (at & 127) * 16;
 #pragma unroll
           for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(dst + i * 4 * 2048) = make_uint4(half2(q[i].x), half2(q[i].y), half2(q[i].z), half2(q[i].w));
         }
       }
-      put(sm + L::kKOff, kr);
-      done(&k_full);
+      put(sm + L::kKOff + (j & 1) * L::kOp, kr);
+      done(&k_full[j & 1]);
       if (j + 1 < total) { known(j + 1); fetch(P.k, N, kr); }
       if (j > 1) { pga_wait(&v_empty[j & 1], (unsigned)((j >> 1) - 1) & 1u, dead, P.err); __syncwarp(); }
       put(sm + L::kVOff + (j & 1) * L::kOp, vr);

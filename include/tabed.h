@@ -425,7 +425,7 @@ typedef struct {
   int32_t dtype;               /* TABED_DTYPE_* of q and out */
   int32_t n_heads;             /* a multiple of n_kv_heads */
   const void *q;               /* [n_tokens][n_heads][head_dim], rows q_stride elements apart */
-  void *out;                   /* the same, rows out_stride elements apart */
+  void *out;                   /* the same, rows out_stride elements apart; may be q itself (and its stride) */
   int64_t q_stride, out_stride;
   float scale;                 /* > 0, of the products q k */
   float softcap;               /* 0, or the cap c: scores become c tanh(score / c) */

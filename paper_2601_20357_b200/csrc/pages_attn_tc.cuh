@@ -123,7 +123,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
   __shared__ uint64_t i_full[kPtInfo], i_empty[kPtInfo], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2];
   __shared__ PtTile info[kPtInfo];
   __shared__ PgaShare s_share;
-  __shared__ float s_cr[128 * MT];               // 1 / scale of the query rows
+  // 1 / scale of the query rows, of four items: an item may be one chunk, and the conversion is up to two chunks ahead of the softmax
+  __shared__ float s_cr[4][128 * MT];
   __shared__ float s_top[2][2][128];             // MT = 1: the largest exponents of both halves of the positions
   __shared__ float2 s_ml[2][128];                // ... and (maximum, sum) at an item's end
   __shared__ uint32_t s_tmem;
@@ -275,6 +276,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     const int piece = lane / RS % NP, row0 = cw * 16 + lane % RS;
     const bool works = NP > 1 || lane < 16;       // (a row of 32 bytes: 16 lanes)
     const bool vec = A.vec_q;
+    int item = -1;
     Row32 kr[NI], vr[NI];
     auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NI]) {
       const int page = T.page[cw], j = T.j0 + cw * 16;
@@ -314,6 +316,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       if (T.first) {                              // the item's query rows (once all scores of the item before are done): a lane has every fourth 16-byte piece of 8 rows a
                                                   // step, so that four lanes read 64 bytes of a row
         if (j > 0) { pga_wait(&k_empty[(j - 1) & 1], (unsigned)((j - 1) >> 1) & 1u, dead, P.err); __syncwarp(); }
+        ++item;
         const int nr = T.nq * grp;
 #pragma unroll 1
         for (int step = 0; step < 2 * MT; ++step) {
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
           // the largest value to 2^14 .. 2^15
           const int ex = min(max((int)(top >> 7) - 127, -100), 127);
           const float up = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-          if (lane < 8) s_cr[at] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
+          if (lane < 8) s_cr[item & 3][at] = __uint_as_float((uint32_t)(127 - 14 + ex) << 23) * 256.0f;
           // (dims whose codes are shifted: 2^8 more; they are the second 16 of every 32, lanes 16 on)
           const float u = lane >= 16 ? up : up * (1.0f / 256.0f);
           auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * u, __uint_as_float(v & 0xFFFF0000u) * u); };
@@ -372,7 +375,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     constexpr int DIMS = MT == 2 ? HD : HD / 2;   // the dims of O that it rescales and writes, from dim0 on
     const int dim0 = half * DIMS;
     float M = kPgaFloor, l = 0.0f, cr = 0.0f, slope = 0.0f;
-    int lim = 0, pos = 0;
+    int lim = 0, pos = 0, item = -1;
     unsigned long long bits = 0;
 #pragma unroll 1
     for (int j = 0; j < total; ++j) {
@@ -384,11 +387,12 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       pt_fence_after();
       const bool first = T.first;
       if (first) {
+        ++item;
         const int rr = T.rt * RB + m * 128 + row % RP, base = T.len - T.nq;
         const bool there = m * 128 + row % RP < RB && rr < T.nq * grp;
         const int i = there ? rr / grp : 0, h = T.kvh * grp + (there ? rr - i * grp : 0);
         M = kPgaFloor; l = 0.0f;
-        cr = s_cr[m * 128 + row] * (cap ? A.scale / A.softcap : A.scale * log2e);
+        cr = s_cr[item & 3][m * 128 + row] * (cap ? A.scale / A.softcap : A.scale * log2e);
         pos = base + i;
         lim = there ? max(0, max(A.tree ? base : min(T.len, base + i + 1), T.pre)) : 0;
         slope = there && A.slopes ? A.slopes[h] * log2e : 0.0f;

@@ -444,6 +444,21 @@ def test_attention_of_one_long_sequence_among_short_ones():
         check_attention(c, p, 0, queries(first[-1], 4, 64, 7), first, [9000, 3, 40])
 
 
+def test_attention_of_many_items_of_one_chunk():
+    """Every item (sequence and KV head) is one chunk, and a CTA has several: their rows differ in size by powers of two, so that an
+    item that took another's scale would show."""
+    n = 120
+    length, rows = [100 + i % 29 for i in range(n)], [17 + i % 4 for i in range(n)]
+    c = make(length, L=1, Hkv=8, ps=128, hd=64, seed=12)
+    first = np.concatenate([[0], np.cumsum(rows)]).tolist()
+    q = queries(first[-1], 8, 64, 11)
+    for e in range(n):
+        q[first[e]:first[e + 1]] *= 2.0 ** -(e % 7) * np.exp2(-np.arange(8) % 5)[None, :, None]
+    p = to_gpu(c)
+    for _ in range(3):
+        check_attention(c, p, 0, q, first, length)
+
+
 def test_attention_names_a_sequence_more_than_once_and_in_any_order():
     c = make([100, 50, 7], Hkv=1, ps=16, hd=32, seed=3)
     p = to_gpu(c)

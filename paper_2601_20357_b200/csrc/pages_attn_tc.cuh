@@ -23,7 +23,7 @@ constexpr int kPtChunk = 128;
 constexpr int kPtStart = 2;                    // chunks that an item's beginning and end cost
 constexpr int kPtInfo = 8;                     // chunks that are known ahead
 constexpr int kPtMaxCtas = 160, kPtMaxRows = 256;
-constexpr size_t kPtSmem = 200u * 1024u;       // (the SM's tensor memory is this CTA's, so its shared memory is too: proj_plan.h, tc_least_smem)
+constexpr size_t kPtSmem = 213u * 1024u;       // (too much for any other CTA with tensor memory beside it, which would wait for columns: proj_plan.h, tc_least_smem)
 
 struct PtTile {
   int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, gaps;      // gaps: positions without a page

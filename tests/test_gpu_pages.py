@@ -151,6 +151,22 @@ def test_append_rotates_by_several_axes(counts, hd, ps, H, Hkv, sections, dtype)
     assert p.last_error() == 0 and p2.last_error() == 0
 
 
+def test_append_turns_by_the_whole_angle():
+    """Unit vectors come back as (cos, sin) themselves.  Allowed: 1 ulp of the fp32 function (2^-24 below 1), half a step of its correction (2^-25), and
+    2^-35 for the correction's own roundings and the reference's angle (turns up to 2^15 in 53 bits: 2^-38 times 2 pi)."""
+    hd, T = 64, 4000
+    p = to_gpu(make([1, 4100], L=1, Hkv=1, ps=64, hd=hd))
+    pos = np.random.default_rng(9).integers(0, 1 << 17, T)
+    q = torch.zeros((T, 1, hd), device=DEV)
+    q[..., :hd // 2] = 1.0
+    out = torch.empty_like(q)
+    p.append(0, q, q, ints([1]), ints([0, T]), ints([0]), T, positions=ints([pos.tolist()]), sections=(hd // 2,), q=q, q_out=out)
+    assert p.last_error() == 0
+    angle = pos[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)
+    want = np.concatenate([np.cos(angle), np.sin(angle)], -1)
+    assert np.abs(out[:, 0].double().cpu().numpy() - want).max() <= 1.5 * 2.0 ** -24 + 2.0 ** -35
+
+
 def test_append_scales_at_the_borders():
     """Maxima at 448 2^e and just behind, subnormal and the largest values, zeros; NaN is stored as 0 and infinities saturate, and
     both are reported."""

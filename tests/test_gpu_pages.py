@@ -2,6 +2,9 @@
 attention, each at the sizes and masks where it can go wrong, what they refuse, and a run of them together."""
 import ctypes as C
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -721,6 +724,75 @@ def test_steps_captured_in_graphs_that_share_a_workspace():
             assert torch.equal(out, w)
             same(from_gpu(p), cache)
             assert p.last_error() == 0
+
+
+FIRST_CALLS = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+import test_gpu_pages as T
+c, st = T.make([400, 190], L=1, Hkv=2, ps=64, hd=64), torch.cuda.Stream()
+outs = []
+for captured in (True, False):
+    p = T.to_gpu(c, stream=st)
+    q = (torch.arange(2 * 30 * 4 * 64, device=T.DEV).reshape(60, 4, 64) %% 7 - 3.0).bfloat16()
+    out, few = torch.zeros_like(q), torch.zeros_like(q[:2])
+    a = [T.ints(x) for x in ([0, 30, 60], [50, 50], [80, 80], [0, 1, 2], [0], [1], [51])]
+    kv = q[:, :2].contiguous()
+    def run():
+        p.append(0, kv, kv, None, a[0], a[1], 30)
+        p.attention(0, q, out, None, a[0], a[2], 30, scale=0.1)
+        p.attention(0, q[:2], few, None, a[3], a[2], 1, scale=0.1)
+        p.compact(a[4], a[1][:1], a[5], a[6].view(1, 1))
+        p.fork(a[4], a[4], a[1][:1], a[2][:1])
+    torch.cuda.synchronize()
+    if captured:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            run()
+        g.replay()
+    else:
+        run()
+    torch.cuda.synchronize()
+    assert p.last_error() == 0
+    outs.append((out, few, T.from_gpu(p)))
+assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+T.same(outs[0][2], outs[1][2])
+"""
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % (os.path.dirname(here), here)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [6, 20, 70, 150])
+def test_query_rows_that_are_not_finite_reach_no_others(rows, dtype):
+    p = to_gpu(make([700], L=1, Hkv=2))
+    q = torch.from_numpy(queries(rows, 4, 64)).to(DEV, TYPES[dtype])
+    odd = q.clone()
+    odd[1, 0, 3], odd[2, 1, 5] = float("nan"), float("inf")
+    outs = []
+    for x in (q, odd):
+        outs.append(torch.empty_like(x))
+        p.attention(0, x, outs[-1], None, ints([0, rows]), ints([700]), rows, scale=0.1)
+    differ = (outs[0] != outs[1]).any(-1)
+    assert differ[1, 0] and differ[2, 1] and differ.sum() == 2 and outs[1][1, 0].isnan().any() and p.last_error() == 0
+
+
+def test_empty_batches():
+    c = make([100, 30])
+    p, z = to_gpu(c), ints([])
+    q, k = torch.empty((0, 4, 64), device=DEV), torch.empty((0, 2, 64), device=DEV)
+    p.fork(z, z, z, z)
+    p.attention(0, q, q, None, ints([0, 0, 0]), ints([100, 30]), 0, scale=0.1)
+    p.append(0, k, k, None, ints([0, 0]), ints([0]), 0, positions=z.view(1, 0), sections=(32,), q=q, q_out=q)
+    p.compact(z, z, z, z.view(0, 0))
+    p.compact(ints([0]), ints([0]), ints([0]), z.view(1, 0))
+    assert p.last_error() == 0
+    same(from_gpu(p), c)
 
 
 def test_calls_give_the_same_bits_every_time():

@@ -110,6 +110,18 @@ def test_nothing_to_do_is_done():
         assert L.tabed_pages_attention(p, C.byref(query(**kw))) == 0
 
 
+def test_nothing_to_do_needs_no_arrays():
+    """The pointer of an empty tensor is null."""
+    L, p = B.lib(), C.byref(pages())
+    none = [None] * 4
+    assert L.tabed_pages_fork(p, *none, 0) == 0 and L.tabed_pages_compact(p, *none, 0, 4) == 0
+    assert L.tabed_pages_compact(p, ADDR, ADDR, ADDR, None, 1, 0) == 0
+    for kw in (dict(n=0), dict(n_tokens=0), dict(max_new=0)):
+        assert L.tabed_pages_append(p, C.byref(new(**kw, k=0, v=0, q=0, q_out=0, positions=0))) == 0
+        assert L.tabed_pages_attention(p, C.byref(query(**kw, q=0, out=0))) == 0
+    assert L.tabed_pages_append(p, C.byref(new(n=0, layer=-1, k=0))) == -1 and L.tabed_pages_fork(p, *none, -1) == -1
+
+
 def test_workspace_grows_with_the_sizes_it_depends_on():
     n = C.c_size_t()
     sizes = []

@@ -211,6 +211,13 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// tanh to 2^-21 of its value: the quotient loses what is small against 1, and a cap far above the scores would multiply that; below 0.3 its
+// Taylor series (the term left out is 5e-8 of it there).
+__device__ __forceinline__ float pga_tanh(float y, float ex2_of_2y) {
+  const float z = y * y;
+  const float s = fmaf(fmaf(fmaf(0.0218694885f, z, -0.0539682540f), z, 0.1333333333f), z, -0.3333333333f);
+  return fabsf(y) < 0.3f ? fmaf(s * z, y, y) : 1.0f - 2.0f * rcp_approx(1.0f + ex2_of_2y);
+}
 // bounded wait of a warp; false if it ran out (recorded)
 __device__ __forceinline__ bool pga_wait(uint64_t* bar, unsigned parity, volatile int* dead, int* err) {
   unsigned spins = 0;
@@ -443,7 +450,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
 #pragma unroll
           for (int j = 0; j < NX; ++j) {
             float z = s[gg][a][j] * (cr[j >> 1] * m.x);
-            if (cap) z = (A.softcap * log2e) * (1.0f - 2.0f * rcp_approx(1.0f + ex2_approx(z * (2.0f * log2e))));      // tanh
+            if (cap) z = (A.softcap * log2e) * pga_tanh(z, ex2_approx(z * (2.0f * log2e)));
             z -= slope[j >> 1] * fabsf((float)(pos[j >> 1] - (jg + 8 * a + ((j & 1) ? c1 : c0))));
             s[gg][a][j] = z + m.y;
           }

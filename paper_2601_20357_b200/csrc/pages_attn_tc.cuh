@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
               }
             } else {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = c2 * (1.0f - 2.0f * rcp_approx(1.0f + ex2_approx(x[i] * (2.0f * log2e))));
+              for (int i = 0; i < 16; ++i) x[i] = c2 * pga_tanh(x[i], ex2_approx(x[i] * (2.0f * log2e)));
             }
           }
           if (A.slopes) {

@@ -437,6 +437,27 @@ def test_attention_of_capped_biased_and_masked_scores(kind, hd, ps, H, Hkv, dtyp
     assert p.last_error() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 4, 40, 100])
+@pytest.mark.parametrize("cap", [1e3, 1e6])
+def test_attention_caps_far_above_the_scores(cap, rows, dtype):
+    """Such a cap changes little, and what it costs must not grow with it: check_attention's bound without the cap among its terms, and as
+    much again of the scores for tanh (2^-21 of its value) and the four products around it (2^-24 each)."""
+    H, hd, length = 4, 64, [300, 117]
+    c = make(length, L=1, Hkv=1, seed=6, nan_tail=True)
+    p = to_gpu(c)
+    q = torch.from_numpy(queries(2 * rows, H, hd, 4)).to(DEV, TYPES[dtype])
+    out = torch.empty_like(q)
+    p.attention(0, q, out, None, ints([0, rows, 2 * rows]), ints(length), rows, scale=0.125, softcap=cap)
+    for e, n in enumerate(length):
+        a, b = e * rows, (e + 1) * rows
+        want, size, terms = O.attention(q[a:b].double().cpu().numpy(), O.gather(c, 0, e, n, "k"), O.gather(c, 0, e, n, "v"), 0.125, O.seen(rows, n, 0, None), cap)
+        weight = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22
+        tol = HALF[dtype] * np.abs(want) + size * (weight + 4 * (terms - cap) * 2.0 ** -20 + 2.0 ** -22 + n * 2.0 ** -27)
+        assert (np.abs(out[a:b].double().cpu().numpy() - want) <= tol).all(), (e, float((np.abs(out[a:b].double().cpu().numpy() - want) / tol).max()))
+    assert p.last_error() == 0
+
+
 def test_attention_where_scales_differ_widely_between_pages():
     """K and V of some pages a thousand times those of others, scores far apart, and a scale that is no power of two."""
     c = make([500], Hkv=2, ps=16, hd=64, seed=4)

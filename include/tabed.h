@@ -350,7 +350,9 @@ int tabed_static_last_error(int32_t device, void* stream);
  *
  * A value is code * scale: the code is e4m3 (4 bits of precision, at most 448 in size, no infinities), the scale belongs to a
  * page, layer and KV head, K and V each their own.  tabed_pages_append and tabed_pages_compact choose scales 2^e, so that
- * bringing codes to another scale is exact (but for values below 2^-6 of the new scale); the attention takes any positive one.
+ * bringing codes to another scale is exact (but for values below 2^-6 of the new scale).  The attention takes any positive one, powers of two
+ * or not; V of a scale below 2^-72 counts as zeros, and the sum of weights leaves out those below 2^-63 S of a row's largest, S being
+ * the largest scale of V that the row sees.
  *
  * `err` is a word on the device, zero at first, in which the calls record what they find in arrays that only the device sees;
  * what such an entry asked for is not done, other entries of the call are.  tabed_pages_last_error names it:

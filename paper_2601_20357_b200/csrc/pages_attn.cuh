@@ -16,7 +16,7 @@
 //     (WR = 1, 2 or 4 tiles of rows a CTA): with up to 16 rows the warps share them and meet at the end of a segment.
 // Numbers.  q is scaled by a power of two per row and rounded to fp16: exact for bf16 values; fp32 rows take a second term (22 bits).
 // With v's scale inside the exponent, w_j = 2^(s_j log2 e + log2 vs_j - M), the sum of w V needs no scale and the sum of
-// weights is that of w_j / vs_j.  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
+// weights is that of w_j / vs_j (a page of zeros has vs = 2^-126: kPgaLeastV).  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
 // M only moves when a score exceeds it by more than 6, so the sums are rarely rescaled.
 // Sequences that span CTAs are put together by k_pages_attn_join from the partial results, in fixed order.
 //
@@ -237,6 +237,16 @@ template <> struct PgaBytes<16> {
   __device__ __forceinline__ void load(const uint8_t* p) { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
 };
 
+// V of a scale below this counts as zero, and log2 of the scale in the exponents stops here.  With s the least scale there and S the largest that a
+// row sees, the sum of weights is 2^15 / s a position at most (2^31 of them: 2^118), and what ex2 flushes in it is below 2^-135 S / s of the
+// largest weight (2^-63 S): with s = 2^-126, a page of zeros, the one was infinite and the other as large as the weights.
+constexpr float kPgaLeastV = 0x1p-72f, kPgaLeastLog = -72.0f;
+// of 16 positions: scale of k, log2 of v's scale, 1 / it
+__device__ __forceinline__ float4 pga_meta(float ks, float vs, bool there) {
+  const float lv = fmaxf(lg2_approx(vs), kPgaLeastLog);
+  return there ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+}
+
 constexpr float kPgaFloor = -1e30f;              // the running maximum of a row that has seen nothing
 constexpr float kPgaSlack = 6.0f, kPgaLift = 9.0f;       // weights are at most 2^(slack + lift) = 2^15
 
@@ -251,7 +261,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
   float* so = reinterpret_cast<float*>(pga_smem_raw + NS * STAGE);        // [slices][rows][HD] states of the warps at a segment's end
   float* sml = so + pga_state_rows<HD, R8>() * HD;                                      // [slices][rows][2]
   __shared__ uint64_t full[NS], empty[NS];
-  __shared__ float4 meta[NS][CH / 16];           // of 16 positions: scale of k, log2 of v's scale, 1 / it
+  __shared__ float4 meta[NS][CH / 16];           // (pga_meta)
   __shared__ PgaShare s_share;
   __shared__ int s_dead;
   const PagesDev& P = A.P;
@@ -275,6 +285,7 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
     int cb = -1, ce = -1, ck = -1;               // block that lane 0 has looked up, entry, KV head
     int pg = -1;
     float pks = 1.0f, pvs = 1.0f;
+    unsigned none = 0;                           // blocks from cb on whose V is not there or counts as zero
     const int ppc = ps < CH ? CH / ps : 1;       // pages of a chunk
     const int rows = ps < CH ? ps : CH;          // positions that it takes of each
     bool ok = true;
@@ -295,32 +306,37 @@ __global__ void __launch_bounds__(kPgaThreads) k_pages_attn(const PagesAttnArgs 
           const size_t at = ((size_t)A.layer * P.NP + pg) * Hkv + w.kvh;
           pks = P.k_scale[at]; pvs = P.v_scale[at];
         }
+        none = __ballot_sync(FULL, pg == -2 || (pg >= 0 && pvs < kPgaLeastV));
       }
       const int mypg = __shfl_sync(FULL, pg, min(blk0 + lane - cb, 31) & 31);
-      const bool has = lane < ppc && blk0 + lane < nblk && mypg >= 0;
-      const unsigned bytes = (unsigned)rows * HD, n_has = __popc(__ballot_sync(FULL, has));
+      const bool inside = lane < ppc && blk0 + lane < nblk, no_v = inside && ((none >> ((blk0 + lane - cb) & 31)) & 1u);
+      const bool has = inside && mypg >= 0, has_v = has && !no_v;
+      const unsigned bytes = (unsigned)rows * HD, copies = __popc(__ballot_sync(FULL, has)) + __popc(__ballot_sync(FULL, has_v));
       unsigned char* sk = ring + st * STAGE;
       {
         const int src = (((p0 + lane * 16) >> P.ls) - cb) & 31;       // (lanes beyond the chunk's groups read something and drop it)
         const float ks = __shfl_sync(FULL, pks, src), vs = __shfl_sync(FULL, pvs, src);
         const int gp = __shfl_sync(FULL, pg, src);
-        if (lane < CH / 16) {
-          const float lv = fmaxf(lg2_approx(vs), -126.0f);
-          meta[st][lane] = gp >= 0 ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
-        }
+        if (lane < CH / 16) meta[st][lane] = pga_meta(ks, vs, gp >= 0);
       }
-      if (lane < ppc && blk0 + lane < nblk && mypg < 0) {       // no page: nothing there, and nothing stale either
-        for (unsigned i = 0; i < 2 * bytes; i += 16)
-          *reinterpret_cast<uint4*>(sk + (i < bytes ? lane * bytes + i : (unsigned)CH * HD + lane * bytes + i - bytes)) = make_uint4(0, 0, 0, 0);
+      if (none) {                                // zeros where no copy comes (K too, where there is no page: nothing stale)
+        for (unsigned left = __ballot_sync(FULL, no_v); left; left &= left - 1) {
+          const unsigned b = __ffs(left) - 1;
+          for (unsigned i = lane * 16; i < bytes; i += 512) *reinterpret_cast<uint4*>(sk + CH * HD + b * bytes + i) = make_uint4(0, 0, 0, 0);
+        }
+        for (unsigned left = __ballot_sync(FULL, inside && mypg < 0); left; left &= left - 1) {
+          const unsigned b = __ffs(left) - 1;
+          for (unsigned i = lane * 16; i < bytes; i += 512) *reinterpret_cast<uint4*>(sk + b * bytes + i) = make_uint4(0, 0, 0, 0);
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       __syncwarp();
-      if (lane == 0) { if (n_has) mbar_expect_tx(&full[st], 2 * n_has * bytes); else mbar_arrive(&full[st]); }
+      if (lane == 0) { if (copies) mbar_expect_tx(&full[st], copies * bytes); else mbar_arrive(&full[st]); }
       __syncwarp();
       if (has) {
         const size_t at = (((size_t)A.layer * P.NP + mypg) * Hkv + w.kvh) * ps * HD + (size_t)(ps > CH ? p0 & (ps - 1) : 0) * HD;
         bulk_g2s(sk + lane * bytes, P.k + at, bytes, &full[st]);
-        bulk_g2s(sk + CH * HD + lane * bytes, P.v + at, bytes, &full[st]);
+        if (has_v) bulk_g2s(sk + CH * HD + lane * bytes, P.v + at, bytes, &full[st]);
       }
       if (c + 1 < total) w.step(A, grp);
     }

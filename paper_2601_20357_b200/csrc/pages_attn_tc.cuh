@@ -32,8 +32,8 @@ constexpr size_t kPtSmem = 213u * 1024u;       // (too much for any other CTA wi
 
 struct PtTile {
   int first, ends, whole, slot, to_end, j0, lim_min, lim_max, q0, nq, len, pre, rt, kvh, e, gaps;      // gaps: positions without a page
-  int page[8];                                 // of 16 positions each; -1: none
-  float4 meta[8];                              // scale of k, log2 of v's scale, 1 / it
+  int k_page[8], v_page[8];                    // of 16 positions each; -1: none, zeros
+  float4 meta[8];                              // (pga_meta)
 };
 
 template <int HD, int MT> struct Pt {
@@ -192,9 +192,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       PtTile& T = info[c % kPtInfo];
       if (c >= kPtInfo) { ok = pga_wait(&i_empty[c % kPtInfo], (unsigned)(c / kPtInfo - 1) & 1u, dead, P.err); ok = __all_sync(FULL, ok); if (!ok) break; }
       if (lane < 8) {
-        const float lv = fmaxf(lg2_approx(vs), -126.0f);
-        T.page[lane] = gp;
-        T.meta[lane] = gp >= 0 ? make_float4(ks, lv, ex2_approx(-lv), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        T.k_page[lane] = gp; T.v_page[lane] = vs < kPgaLeastV ? -1 : gp;
+        T.meta[lane] = pga_meta(ks, vs, gp >= 0);
       }
       if (fresh) from_start = w.ch == 0;
       const bool gaps = __any_sync(FULL, lane < 8 && gp < 0);
@@ -283,8 +282,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     const bool vec = A.vec_q;
     int item = -1;
     Row32 kr[NI], vr[NI];
-    auto fetch = [&](const uint8_t* codes, const PtTile& T, Row32 (&r)[NI]) {
-      const int page = T.page[cw], j = T.j0 + cw * 16;
+    auto fetch = [&](const uint8_t* codes, const int (&pages)[8], const PtTile& T, Row32 (&r)[NI]) {
+      const int page = pages[cw], j = T.j0 + cw * 16;
       const uint8_t* p = codes + (((size_t)A.layer * P.NP + max(page, 0)) * Hkv + T.kvh) * (ps * HD) + ((j & (ps - 1)) + lane % RS) * HD + piece * 32;
       const int live = page >= 0 ? T.lim_max - j - lane % RS : 0;      // (what nobody sees becomes zeros: 0 * NaN is not 0)
 #pragma unroll
@@ -310,8 +309,8 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
     auto done = [&](uint64_t* bar) { pt_fence_async(); __syncwarp(); if (lane == 0) mbar_arrive(bar); };
     if (total > 0) {
       known(0);
-      fetch(P.k, info[0], kr);
-      fetch(P.v, info[0], vr);
+      fetch(P.k, info[0].k_page, info[0], kr);
+      fetch(P.v, info[0].v_page, info[0], vr);
     }
 #pragma unroll 1
     for (int j = 0; j < total; ++j) {
@@ -365,11 +364,11 @@ __global__ void __launch_bounds__(Pt<HD, MT>::kThreads, 1) k_pages_attn_tc(const
       }
       put(sm + L::kKOff + (j & 1) * L::kOp, kr);
       done(&k_full[j & 1]);
-      if (j + 1 < total) { known(j + 1); fetch(P.k, N, kr); }
+      if (j + 1 < total) { known(j + 1); fetch(P.k, N.k_page, N, kr); }
       if (j > 1) { pga_wait(&v_empty[j & 1], (unsigned)((j >> 1) - 1) & 1u, dead, P.err); __syncwarp(); }
       put(sm + L::kVOff + (j & 1) * L::kOp, vr);
       done(&v_full[j & 1]);
-      if (j + 1 < total) fetch(P.v, N, vr);
+      if (j + 1 < total) fetch(P.v, N.v_page, N, vr);
     }
   } else if (warp < W_CONV) {
     // ---- softmax ----

@@ -379,9 +379,10 @@ int tabed_pages_workspace(const tabed_pages* p, size_t* bytes);
 
 /* Copy, fork, cut, grow and free sequences: for each of n entries, sequence dst becomes the first keep tokens of sequence src,
  * with room for len >= keep tokens.  The pages that the kept tokens fill are shared; where keep ends inside a page, dst gets a
- * page of its own with copies of those tokens and of the scales, in all layers (src == dst: the page itself, if nobody else names it).  Blocks up to len get
- * free pages, the lowest-numbered ones in the order of (entry, block); entries of dst's table beyond are -1, and the pages that
- * it named before are given back.  src == dst grows (keep = the tokens it holds) or cuts a sequence, keep = len = 0 frees it.
+ * page of its own with copies of those tokens and of the scales, in all layers (src == dst: the page itself, if nobody else names it
+ * once all entries have given theirs back; of several entries of which this holds, the first).  Blocks up to len get free pages,
+ * the lowest-numbered ones in the order of (entry, block); entries of dst's table beyond are -1, and the pages that it named before are
+ * given back.  src == dst grows (keep = the tokens it holds) or cuts a sequence, keep = len = 0 frees it.
  * All entries see tables and caches as they were before the call, and pages given back by it are free for it.  An entry that
  * runs out of pages has -1 in their place (KV_OVERFLOW).
  * src, dst, keep, len: int32 [n], n <= n_seqs, every dst once.  Every block of src's kept tokens must have a page (INVALID_ARG). */

@@ -140,7 +140,12 @@ def fork(cache, src, dst, keep, length):
         for page in old[d]:
             if page >= 0:
                 named[page] -= 1
-    stays = [bool(n % ps) and s == d and named[old[s, n // ps]] == 0 for s, d, n in zip(src, dst, keep)]
+    stays, claimed = [], set()                                  # of several that nobody but they named, the first entry keeps the page
+    for s, d, n in zip(src, dst, keep):
+        tail = int(old[s, n // ps]) if n % ps else -1
+        stays.append(tail >= 0 and s == d and named[tail] == 0 and tail not in claimed)
+        if stays[-1]:
+            claimed.add(tail)
     pinned = {int(old[s, n // ps]) for s, d, n in zip(src, dst, keep) if n % ps}
     free = [p for p in range(len(ref)) if named[p] == 0 and p not in pinned]
     enough = True

@@ -18,7 +18,7 @@ using namespace tabed;
 namespace {
 
 constexpr int kMaxDevices = 64;
-constexpr int kMaxPageSeqs = 32767;       // references and pins share a word of `ref` while a fork runs
+constexpr int kMaxPageSeqs = 32767;       // counts of references and of entries share a word of `ref` while a fork runs
 
 struct OnDevice {
   int prev = -1; bool ok = true;

@@ -340,11 +340,11 @@ __global__ void __launch_bounds__(128) k_pages_load_row(const PagesDev P, int se
 }
 
 // ---- fork ------------------------------------------------------------------------------------------
-// Three launches: the references of the pages shared, pinned and given back (a CTA an entry; atomic additions, whose order does
+// Three launches: the references of the pages shared, marked and given back (a CTA an entry; atomic operations whose order does
 // not matter), the free pages (one CTA: who needs how many, and the lowest-numbered ones in order), the tables and the copies.  The
 // first two are one CTA's launch for few and short tables.
-// While the call runs a page's word in `ref` holds its references in the low half and in the high half how many entries copy from
-// it: such a page is not handed out even where nobody names it any longer.
+// While the call runs a page's word in `ref` holds its references in the low half, above them how many entries keep a part of it in place (src
+// == dst), and in the sign whether others copy from it: such a page is not handed out even where nobody names it any longer.
 struct ForkEntry { int valid, stays, first_new, tail; };     // tail: page of the block that keep ends in, -1 if it ends with a block
 
 struct ForkArgs {
@@ -359,6 +359,9 @@ struct ForkArgs {
 };
 
 constexpr int kForkThreads = 256;
+constexpr int kForkKeeps = 1 << 16, kForkCopies = (int)0x80000000;
+__device__ __forceinline__ void fork_mark(int* word, bool keeps) { if (keeps) atomicAdd(word, kForkKeeps); else atomicOr(word, kForkCopies); }
+__device__ __forceinline__ void fork_unmark(int* word, bool keeps) { if (keeps) atomicAdd(word, -kForkKeeps); else atomicAnd(word, ~kForkCopies); }
 constexpr int kForkAllocThreads = 1024;
 
 __global__ void __launch_bounds__(kForkThreads) k_pages_share(const ForkArgs A) {
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(kForkThreads) k_pages_share(const ForkArgs A) 
     row[b] = pg;
     atomicAdd(P.ref + pg, 1);
   }
-  if (tid == 0 && part > 0) atomicAdd(P.ref + from[full], 1 << 16);
+  if (tid == 0 && part > 0) fork_mark(P.ref + from[full], src == dst);
   const int* to = P.table + (size_t)dst * P.max_pages;
   for (int b = tid; b < P.max_pages; b += kForkThreads) {
     const int pg = to[b];
@@ -417,27 +420,45 @@ __device__ __forceinline__ int block_scan(int v, int* s_scan, int* total) {
 }
 
 // Who needs how many pages, and the free ones in order: one CTA.
+// An entry that keeps a part of its own page stays in it if nobody names the page after all have given theirs back; of several that were cut
+// inside a page they shared, the first stays and the others copy.  Where there are such, they bid for the page in its word's low half, which is
+// 0: 0xFFFF - entry, above any count of references; the largest is the first entry's.
 __device__ __forceinline__ void fork_alloc(const ForkArgs& A, int* s_scan) {
   const PagesDev& P = A.P;
   const int tid = threadIdx.x;
+  int shared = 0;
+  for (int e = tid; e < A.n; e += kForkAllocThreads) {
+    const ForkEntry E = A.ent[e];
+    if (!E.valid || E.tail < 0 || A.src[e] != A.dst[e]) continue;
+    const int w = __ldcg(P.ref + E.tail);
+    if ((w & 0xFFFF) != 0) continue;
+    A.ent[e].stays = 1;
+    shared |= (w & ~kForkCopies) >= 2 * kForkKeeps;
+  }
+  const bool bids = __syncthreads_or(shared) != 0;
+  if (bids) {
+    for (int e = tid; e < A.n; e += kForkAllocThreads)
+      if (A.ent[e].stays) {
+        int* word = P.ref + A.ent[e].tail;
+        atomicMax(word, (__ldcg(word) & ~0xFFFF) | (0xFFFF - e));
+      }
+    __syncthreads();
+    for (int e = tid; e < A.n; e += kForkAllocThreads)
+      if (A.ent[e].stays) A.ent[e].stays = (__ldcg(P.ref + A.ent[e].tail) & 0xFFFF) == 0xFFFF - e;
+  }
   int need_all = 0;
   for (int base = 0; base < A.n; base += kForkAllocThreads) {
     const int e = base + tid;
     int need = 0;
-    if (e < A.n && A.ent[e].valid) {
-      const int keep = A.keep[e], full = keep / P.ps, tail = A.ent[e].tail;
-      const int stays = tail >= 0 && A.src[e] == A.dst[e] && (__ldcg(P.ref + tail) & 0xFFFF) == 0;
-      need = (A.len[e] + P.ps - 1) / P.ps - full - stays;
-      A.ent[e].stays = stays;
-    }
+    if (e < A.n && A.ent[e].valid) need = (A.len[e] + P.ps - 1) / P.ps - A.keep[e] / P.ps - A.ent[e].stays;
     int total;
     const int before = block_scan(need, s_scan, &total);
     if (e < A.n) A.ent[e].first_new = need_all + before;
     need_all += total;
   }
-  // (every decision above has been taken: the pages that stay with their sequence get their reference)
+  // (every bid has been read: the pages that stay with their sequence get their reference)
   for (int e = tid; e < A.n; e += kForkAllocThreads)
-    if (A.ent[e].valid && A.ent[e].stays) atomicAdd(P.ref + A.ent[e].tail, 1);
+    if (A.ent[e].valid && A.ent[e].stays) atomicAdd(P.ref + A.ent[e].tail, bids ? 1 - (0xFFFF - e) : 1);
   __syncthreads();
   constexpr int PER = 8;
   int found = 0;
@@ -505,7 +526,7 @@ __global__ void __launch_bounds__(kForkAllocThreads) k_pages_plan(const ForkArgs
     const int keep = s_keep[tid], tail = bad || (keep & (P.ps - 1)) == 0 ? -1 : P.table[(size_t)s_src[tid] * W + (keep >> P.ls)];
     A.ent[tid] = ForkEntry{!bad, 0, 0, tail};
     if (bad) atomicOr(P.err, over ? PERR_KV : PGERR_INVALID);
-    if (tail >= 0) atomicAdd(P.ref + tail, 1 << 16);
+    if (tail >= 0) fork_mark(P.ref + tail, s_src[tid] == s_dst[tid]);
   }
   for (int i = tid; i < A.n * W; i += kForkAllocThreads) {
     const int e = i / W, b = i - e * W;
@@ -544,7 +565,7 @@ __global__ void __launch_bounds__(kForkThreads) k_pages_settle(const ForkArgs A)
       }
       to[b] = pg;
     }
-    if (tid == 0 && E.tail >= 0) atomicAdd(P.ref + E.tail, -(1 << 16));
+    if (tid == 0 && E.tail >= 0) fork_unmark(P.ref + E.tail, A.src[e] == A.dst[e]);
     return;
   }
   if (E.tail < 0 || E.stays || E.first_new >= found) return;

@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
     return;
   }
   const int p1 = p0 + (f1 - f0), bi = (p0 >> P.ls) + slot;
-  if (f1 == f0 || bi * ps >= p1) return;
+  if (f1 == f0 || slot > ((p1 - 1) >> P.ls) - (p0 >> P.ls)) return;      // (not by bi * page_tokens, which may pass 2^31)
   const int lo = max(p0, bi * ps), cnt = min(p1, (bi + 1) * ps) - lo, off = lo - bi * ps, t0 = f0 + (lo - p0);
   const int u0 = blockIdx.y * A.hpc, u1 = min(u0 + A.hpc, 2 * P.Hkv + (A.has_q ? A.n_heads : 0));
   const int lt = 31 - __clz(hd >> 4), n_items = cnt << lt;      // hd / 16 = 2^lt items a token

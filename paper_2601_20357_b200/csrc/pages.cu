@@ -318,7 +318,7 @@ int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {
   const long long rows = (long long)t->max_new * (t->n_heads / p->n_kv_heads);
   a.WR = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
   a.RB = rows <= 8 ? 8 : 16 * a.WR;
-  if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFFF0ll) return TABED_ERR_UNSUPPORTED;      // (an entry's rows are counted in 31 bits)
+  if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFF00ll) return TABED_ERR_UNSUPPORTED;      // (an entry's rows, up to the end of a tile of 256, are counted in 31 bits)
   a.part_rows = kPgaMaxRows;
   if (t->dtype == TABED_DTYPE_BF16 && rows > 16) {
     a.RB = rows <= 64 ? 64 : (rows <= 128 ? 128 : 256);

@@ -457,7 +457,8 @@ int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t*
  * that wait), and rows are filled from a sequence (after tabed_pages_fork: the same prompt under several inputs).  Both run on
  * the handle's stream, on caches of its drafter's layers, KV heads, head size and device; what a row is filled with went through 8 bits.
  * tabed_pages_store_row writes the positions start .. start + len - 1 of the row to those of sequence seq, as tabed_pages_append does (no
- * rotation: a row's keys are rotated already).  tabed_pages_load_row makes the first len tokens of the sequence the row's committed cache.
+ * rotation: a row's keys are rotated already); positions that the row has not committed are refused, on the host where it knows (INVALID_ARG), else on
+ * the device (nothing is written, INVALID_ARG in p->err).  tabed_pages_load_row makes the first len tokens of the sequence the row's committed cache.
  * Errors: NULL_PTR, BAD_STATE (mid-round, handle without drafter), INVALID_ARG (sizes that differ, row, seq or tokens out of range), KV_OVERFLOW (beyond
  * the sequence's blocks); what only the device sees goes to p->err. */
 int tabed_pages_store_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t start, int32_t len);

@@ -190,7 +190,7 @@ int pages_store_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r
   const int hd = p->head_dim;
   const size_t esz = r.f32 ? 4 : 2;
   AppendArgs a = {};
-  a.P = on_device(p); a.n = 1; a.n_tokens = len; a.max_new = len; a.seq0 = seq; a.start0 = start;
+  a.P = on_device(p); a.n = 1; a.n_tokens = len; a.max_new = len; a.seq0 = seq; a.start0 = start; a.held = r.len;
   a.kv_stride = hd; a.kv_head = (long long)r.cap * hd; a.vec_kv = 1;
   for (a.layer = 0; a.layer < p->n_layers; ++a.layer) {
     const size_t at = ((size_t)a.layer * p->n_kv_heads * r.cap + start) * hd * esz;
@@ -202,12 +202,12 @@ int pages_store_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r
   return TABED_OK;
 }
 
-int pages_load_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r, int seq, int len, int* kv_len, int64_t* launches) {
+int pages_load_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r, int seq, int len, int64_t* launches) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((len + p->page_tokens - 1) / p->page_tokens, 2 * p->n_kv_heads, p->n_layers); cfg.blockDim = dim3(128); cfg.stream = stream;
   const PagesDev d = on_device(p);
-  const cudaError_t rc = r.f32 ? cudaLaunchKernelEx(&cfg, k_pages_load_row<float>, d, seq, len, static_cast<float*>(r.k), static_cast<float*>(r.v), r.cap, kv_len)
-                               : cudaLaunchKernelEx(&cfg, k_pages_load_row<__nv_bfloat16>, d, seq, len, static_cast<__nv_bfloat16*>(r.k), static_cast<__nv_bfloat16*>(r.v), r.cap, kv_len);
+  const cudaError_t rc = r.f32 ? cudaLaunchKernelEx(&cfg, k_pages_load_row<float>, d, seq, len, static_cast<float*>(r.k), static_cast<float*>(r.v), r.cap, r.len)
+                               : cudaLaunchKernelEx(&cfg, k_pages_load_row<__nv_bfloat16>, d, seq, len, static_cast<__nv_bfloat16*>(r.k), static_cast<__nv_bfloat16*>(r.v), r.cap, r.len);
   if (rc != cudaSuccess) { cudaGetLastError(); return TABED_ERR_CUDA; }
   ++*launches;
   return TABED_OK;

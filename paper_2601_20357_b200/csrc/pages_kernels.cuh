@@ -57,6 +57,7 @@ struct AppendArgs {
   int layer, n, n_tokens, max_new, n_heads, nblk, hpc, n_axes, has_q;
   const int *seq, *first, *start, *positions;      // seq null: entry e is sequence seq0 + e; first null: one entry, all tokens, from start0 on
   int seq0, start0;
+  const int* held;                    // tokens that the rows come from (null: any number): none behind them are taken
   const void *k, *v, *q;
   void* q_out;
   long long kv_stride, kv_head, q_stride, q_out_stride;      // elements between tokens; between heads of K and V
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
   pdl_wait();
   const int s = A.seq ? A.seq[e] : A.seq0 + e, f0 = A.first ? A.first[e] : 0, f1 = A.first ? A.first[e + 1] : A.n_tokens, p0 = A.start ? A.start[e] : A.start0;
   const int ps = P.ps, hd = P.hd, half = hd >> 1;
-  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens || s < 0 || s >= P.n_seqs || p0 < 0 || f1 - f0 > A.max_new) {
+  if (f0 < 0 || f1 < f0 || f1 > A.n_tokens || s < 0 || s >= P.n_seqs || p0 < 0 || f1 - f0 > A.max_new || (A.held && p0 > *A.held - (f1 - f0))) {
     if (tid == 0) atomicOr(P.err, PGERR_INVALID);
     return;
   }

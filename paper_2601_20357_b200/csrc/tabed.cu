@@ -1163,7 +1163,7 @@ int tabed_load_prefix_kv(tabed_handle* h, int32_t row, const void* k, const void
 
 static DenseRow dense_row(tabed_handle* h, int row) {
   const size_t bytes = (size_t)h->L * h->Hkv * h->cap * h->hd * h->esz;
-  return DenseRow{static_cast<unsigned char*>(h->kc) + row * bytes, static_cast<unsigned char*>(h->vc) + row * bytes, h->cap, h->esz == 4};
+  return DenseRow{static_cast<unsigned char*>(h->kc) + row * bytes, static_cast<unsigned char*>(h->vc) + row * bytes, h->cap, h->esz == 4, h->kv_len + row};
 }
 
 int tabed_pages_store_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t start, int32_t len) {
@@ -1186,7 +1186,7 @@ int tabed_pages_load_row(tabed_handle* h, const tabed_pages* p, int32_t row, int
   if (len > (long long)p->max_pages * p->page_tokens) return TABED_ERR_KV_OVERFLOW;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return TABED_ERR_CUDA;
-  rc = pages_load_row(p, h->stream, dense_row(h, row), seq, len, h->kv_len + row, &h->launches);
+  rc = pages_load_row(p, h->stream, dense_row(h, row), seq, len, &h->launches);
   if (rc == TABED_OK) h->len_ub[row] = len;
   return rc;
 }

@@ -442,10 +442,11 @@ class Pages:
         need = C.c_size_t()
         _check(lib().tabed_pages_workspace(C.byref(p), C.byref(need)), "tabed_pages_workspace")
         self.workspace_bytes = need.value
-        if err is None:
-            err = torch.zeros(1, dtype=torch.int32, device=dev)
-        if workspace is None:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.default_stream(dev)):      # the stream of the calls that use them
+            if err is None:
+                err = torch.zeros(1, dtype=torch.int32, device=dev)
+            if workspace is None:
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
         if workspace.numel() * workspace.element_size() < need.value:
             raise ValueError(f"workspace: expected {need.value} bytes at least")
         p.err, p.workspace = _ptr(err, torch.int32, 1, "err", dev), _ptr(workspace, workspace.dtype, None, "workspace", dev)

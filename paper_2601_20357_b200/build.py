@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
@@ -25,18 +26,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    flags = ["-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a"]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = ["-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo"] + arch
     if verbose:
         flags += ["-Xptxas", "-v"]
-    objects = [os.path.join(CSRC, os.path.splitext(s)[0] + ".o") for s in SOURCES]
-    runs = [subprocess.Popen([nvcc, "-c"] + flags + ["-o", o, os.path.join(CSRC, s)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-            for s, o in zip(SOURCES, objects)]
-    said = [r.communicate()[0] for r in runs]
-    if all(r.returncode == 0 for r in runs):
-        link = subprocess.run([nvcc, "-shared"] + flags[-2:] + ["-o", LIB_PATH] + objects, capture_output=True, text=True)
-        runs, said = runs + [link], said + [link.stdout + link.stderr]
-    if any(r.returncode != 0 for r in runs):
-        raise RuntimeError("nvcc failed:\n" + "".join(said))
+    # Another process may build at the same time: files of this build's own, and the library appears whole.
+    with tempfile.TemporaryDirectory(dir=PKG_DIR, prefix="build") as tmp:
+        objects = [os.path.join(tmp, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+        linked = os.path.join(tmp, os.path.basename(LIB_PATH))
+        runs = [subprocess.Popen([nvcc, "-c"] + flags + ["-o", o, os.path.join(CSRC, s)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                for s, o in zip(SOURCES, objects)]
+        said = [r.communicate()[0] for r in runs]
+        if all(r.returncode == 0 for r in runs):
+            link = subprocess.run([nvcc, "-shared"] + arch + ["-o", linked] + objects, capture_output=True, text=True)
+            runs, said = runs + [link], said + [link.stdout + link.stderr]
+        if any(r.returncode != 0 for r in runs):
+            raise RuntimeError("nvcc failed:\n" + "".join(said))
+        os.replace(linked, LIB_PATH)
     if verbose:
         sys.stderr.write("".join(said))
     return LIB_PATH

@@ -241,7 +241,7 @@ int tabed_pages_fork(const tabed_pages* p, const int32_t* src, const int32_t* ds
   a.free_list = reinterpret_cast<int*>(ws);
   a.vec_ref = aligned(p->ref, 16);
   int rc;
-  if (n <= kPlanEntries && (long long)n * p->max_pages <= kPlanBlocks) {      // (3 entries of 13 blocks 10.3 -> 9.3 us; 96 of 67 would go from 11.9 to 17.4)
+  if (n <= kPlanEntries && (long long)n * p->max_pages <= kPlanBlocks) {      // (15 blocks 9.8 us against 10.6 in three launches, 624 12.0 and 12.6, 1152 13.1 and 12.7, 6336 21.5 and 15.1)
     rc = launch(p, k_pages_plan, dim3(1), kForkAllocThreads, 0, a);
   } else {
     rc = launch(p, k_pages_share, dim3(n), kForkThreads, 0, a);
@@ -345,10 +345,12 @@ int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t*
   if (!guard.ok) return TABED_ERR_CUDA;
   CompactArgs a;
   a.P = on_device(p); a.seq = seq; a.start = start; a.count = count; a.index = index; a.n = n; a.width = width;
-  // A warp a unit where there are many units or few tokens, else four; blocks of more than 4 KB take four.  1024 of 4096 tokens, 8 sequences, 4
-  // layers, 12 heads (768 units): one warp 55 us, four 40; the 6 tokens of 32 trees, 12 layers, 2 heads (1536 units): one 10.2.
+  // A warp a unit where fewer tokens than a page move, else four; blocks of more than 4 KB take four.  Pages of 64 tokens of 64 values, 12 KV
+  // heads, one warp against four: 768 units (sequences, layers, heads, K and V) of 32 tokens 6.0 and 6.6 us, of 128 9.4 and 8.9, of 1024 55 and 40; 5760
+  // units of 512 127 and 102, 9600 of 256 113 and 102.  With few KV heads a CTA's eight warps are not all there, and four are faster
+  // at any number: 1536 units of 2 KV heads, 6 tokens 10.2 and 8.8 (left: the call is bound by its launch and dependent trips).
   const int bytes = p->page_tokens * p->head_dim;
-  const bool one = bytes <= 4096 && (width < p->page_tokens || (long long)n * p->n_layers * 2 * p->n_kv_heads > 32ll * sm_count(p->device));
+  const bool one = bytes <= 4096 && width < p->page_tokens;
   const int per = kCompactThreads / 32 / (one ? 1 : 4);
   const dim3 grid(n, p->n_layers, (2 * p->n_kv_heads + per - 1) / per);
   if (one) return launch(p, k_pages_compact<1, 8>, grid, kCompactThreads, 0, a);

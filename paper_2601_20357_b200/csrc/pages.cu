@@ -313,14 +313,17 @@ int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t) {
   a.seq = t->seq; a.first = t->first; a.length = t->length; a.q = t->q; a.out = t->out; a.q_stride = t->q_stride; a.out_stride = t->out_stride;
   a.scale = t->scale; a.softcap = t->softcap; a.slopes = t->slopes; a.prefix = t->prefix; a.tree = reinterpret_cast<const unsigned long long*>(t->tree);
   a.vec_q = rows_aligned(t->q, t->q_stride, esz) && rows_aligned(t->out, t->out_stride, esz);
-  // Up to 16 rows a KV head, and fp32 rows, multiply from registers (8 rows a tile, or 16 a warp in 1 - 4 warps); more bf16 rows go through
-  // tensor memory in tiles of 64, 128 or 256 rows: 32 trees of 64 rows 434 us there, 162 here; prompt chunks of 2048 tokens 1514 and 267.
+  // Up to 16 rows a KV head (32 of head sizes 32 and 64), and fp32 rows, multiply from registers (8 rows a tile, or 16 a warp in 1 - 4 warps); more
+  // bf16 rows go through tensor memory in tiles of 64, 128 or 256 rows.  Registers and tensor memory, us: 32 sequences of 500 - 8192 tokens, 8 KV
+  // heads of 128, 16 rows 142 and 138, 20 rows 188 and 138, 64 rows 321 and 145; 12 KV heads of 64, 96 sequences of 256 - 4096, 16 rows 113 and
+  // 211, 32 rows 158 and 214, 40 rows 254 and 215; 4 KV heads of 32, 64 sequences, 32 rows 49 and 63, 40 rows 60 and 65; prompt chunks of
+  // 2048 tokens 1514 and 267.  Tiles of 64, 128 and 256 (heads of 128): 64 rows 145, 154, 221, 72 rows 232, 155, 224, 128 rows 259, 162, 228, 136 rows 342, 248, 230.
   const long long rows = (long long)t->max_new * (t->n_heads / p->n_kv_heads);
   a.WR = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
   a.RB = rows <= 8 ? 8 : 16 * a.WR;
   if ((long long)t->n_tokens * (t->n_heads / p->n_kv_heads) > 0x7FFFFF00ll) return TABED_ERR_UNSUPPORTED;      // (an entry's rows, up to the end of a tile of 256, are counted in 31 bits)
   a.part_rows = kPgaMaxRows;
-  if (t->dtype == TABED_DTYPE_BF16 && rows > 16) {
+  if (t->dtype == TABED_DTYPE_BF16 && rows > (hd == 128 ? 16 : 32)) {
     a.RB = rows <= 64 ? 64 : (rows <= 128 ? 128 : 256);
     a.part_rows = kPtMaxRows;
   }

@@ -1,4 +1,4 @@
-// Attention over a paged 8-bit cache for few query rows a KV head (decoding steps, short blocks), and for fp32 rows; more than 16 bf16 rows
+// Attention over a paged 8-bit cache for few query rows a KV head (decoding steps, short blocks), and for fp32 rows; more bf16 rows
 // go to pages_attn_tc.cuh.
 //
 //   out_i = sum_j softmax_j(s_ij) v_j,   s_ij = cap(scale q_i k_j) - slope |pos_i - j|,   k = codes * scale of their page

@@ -1,5 +1,5 @@
-// Attention over a paged 8-bit cache on the fifth-generation tensor cores, for more than 16 bf16 query rows a KV head: token trees, verified
-// blocks, chunks of prompts.  The same list of chunks (here of 128 positions), numbers and partial results as pages_attn.cuh.
+// Attention over a paged 8-bit cache on the fifth-generation tensor cores, for many bf16 query rows a KV head (more than 16, of head sizes 32 and
+// 64 more than 32): token trees, verified blocks, chunks of prompts.  The same list of chunks (here of 128 positions), numbers and partial results as pages_attn.cuh.
 //
 //   S [128 rows][128 positions] = Q K^T        Q, K in shared memory (kind::f16, fp32 sums in tensor memory)
 //   O [128 rows][hd]           += P V          P in tensor memory (over its S), V in shared memory

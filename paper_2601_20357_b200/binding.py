@@ -7,6 +7,7 @@ shared library has not been built, loading fails with an error.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Dict, List, Optional, Sequence
@@ -442,7 +443,8 @@ class Pages:
         need = C.c_size_t()
         _check(lib().tabed_pages_workspace(C.byref(p), C.byref(need)), "tabed_pages_workspace")
         self.workspace_bytes = need.value
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.default_stream(dev)):      # the stream of the calls that use them
+        where = stream if stream is not None else torch.cuda.default_stream(dev)       # the stream of the calls that use them
+        with contextlib.nullcontext() if where == torch.cuda.current_stream(dev) else torch.cuda.stream(where):
             if err is None:
                 err = torch.zeros(1, dtype=torch.int32, device=dev)
             if workspace is None:

@@ -29,7 +29,7 @@
  *   - Embeddings, weights and loaded caches are expected to be finite.  The decode kernels read a row's last tile of
  *     cache positions whole and give the positions beyond its length a weight of zero, so a row that once held
  *     non-finite positions may give NaN again after tabed_state_import took it back to a shorter length, until
- *     tabed_load_prefix_kv or a prompt over those positions replaces them.
+ *     tabed_load_prefix_kv, tabed_pages_load_row or a prompt over those positions replaces them.
  *   - Layouts are row-major with the last index fastest.  B = n_requests, m = n_inputs,
  *     R = B*m rows (row = request*m + input), V = vocab, G = gamma.
  *   - Uniforms are caller-supplied floats on the lattice u = (k + 1/2) * 2^-23, 0 <= k < 2^23.
@@ -392,7 +392,8 @@ int tabed_pages_fork(const tabed_pages* p, const int32_t* src, const int32_t* ds
 typedef struct {
   int32_t layer;
   int32_t n;                   /* entries: sequences that get tokens */
-  int32_t n_tokens, max_new;   /* rows of k, v (and q); no entry has more than max_new of them */
+  int32_t n_tokens, max_new;   /* rows of k, v (and q); no entry has more than max_new of them.  n, n_tokens or max_new of 0: nothing is done,
+                                  no array is looked at */
   const int32_t *seq;          /* [n] sequence of an entry, every one at most once (NULL: entry i is sequence i) */
   const int32_t *first;        /* [n + 1] entry i has the rows first[i] .. first[i + 1] - 1 */
   const int32_t *start;        /* [n] position of its first token in the sequence */
@@ -421,7 +422,8 @@ int tabed_pages_append(const tabed_pages* p, const tabed_pages_new* t);
 typedef struct {
   int32_t layer;
   int32_t n;                   /* entries */
-  int32_t n_tokens, max_new;   /* rows of q; no entry has more than max_new of them (more: INVALID_ARG, zeros) */
+  int32_t n_tokens, max_new;   /* rows of q; no entry has more than max_new of them (more: INVALID_ARG, zeros).  n, n_tokens or max_new of 0:
+                                  nothing is done, no array is looked at */
   const int32_t *seq;          /* [n] sequence of an entry (NULL: entry i is sequence i); a sequence may be named by several */
   const int32_t *first;        /* [n + 1] entry i has the rows first[i] .. first[i + 1] - 1 */
   const int32_t *length;       /* [n] tokens in the sequence, those of the rows themselves (its last ones) included */
@@ -442,7 +444,8 @@ typedef struct {
  * prefix; with a tree the length - r positions before the rows, the prefix, and the rows of its mask.  A row that sees nothing is 0.
  * Pages beyond the length and positions that no row of an entry sees may hold anything; a code that is NaN at a position that
  * some rows of an entry see may reach others of its rows too (tabed_pages_append writes none).  A block without a page counts as not seen (INVALID_ARG).
- * Rows of no entry are left as they are. */
+ * Rows of no entry are left as they are.  The same call gives the same bits every time; in another batch, or with another max_new, a row may be split
+ * and rounded differently, within the same bounds. */
 int tabed_pages_attention(const tabed_pages* p, const tabed_pages_query* t);
 
 /* Keep some tokens of sequences and move them together (a token tree's accepted sibling behind its chain, pruned image tokens),
@@ -460,11 +463,12 @@ int tabed_pages_compact(const tabed_pages* p, const int32_t* seq, const int32_t*
  * rotation: a row's keys are rotated already); positions that the row has not committed are refused, on the host where it knows (INVALID_ARG), else on
  * the device (nothing is written, INVALID_ARG in p->err).  tabed_pages_load_row makes the first len tokens of the sequence the row's committed cache.
  * Errors: NULL_PTR, BAD_STATE (mid-round, handle without drafter), INVALID_ARG (sizes that differ, row, seq or tokens out of range), KV_OVERFLOW (beyond
- * the sequence's blocks); what only the device sees goes to p->err. */
+ * the sequence's blocks); what only the device sees goes to p->err (before tabed_pages_last_error, let p->stream wait for the handle's stream if it is
+ * another one). */
 int tabed_pages_store_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t start, int32_t len);
 int tabed_pages_load_row(tabed_handle* h, const tabed_pages* p, int32_t row, int32_t seq, int32_t len);
 
-/* Synchronises the stream, returns the code of what the calls recorded in `err` since the last time (TABED_OK if nothing), and clears it. */
+/* Synchronises p->stream, returns the code of what the calls recorded in `err` since the last time (TABED_OK if nothing), and clears it. */
 int tabed_pages_last_error(const tabed_pages* p);
 
 /* Stand-alone run of the tensor-core projection used for many shared-weight rows (Sec. 4.1 "batched

@@ -184,6 +184,7 @@ int pages_match(const tabed_pages* p, int L, int Hkv, int hd, int device) {
   return p->n_layers == L && p->n_kv_heads == Hkv && p->head_dim == hd && p->device == device ? TABED_OK : TABED_ERR_INVALID_ARG;
 }
 
+// (a launch a layer: 4 layers of 12 heads of 64, 704 tokens 18 us, 8192 80 us; 12 layers of 2 heads, 4096 tokens 47 us)
 int pages_store_row(const tabed_pages* p, cudaStream_t stream, const DenseRow& r, int seq, int start, int len, int64_t* launches) {
   tabed_pages here = *p;
   here.stream = stream;

@@ -17,11 +17,12 @@
 // Numbers.  q is scaled by a power of two per row and rounded to fp16: exact for bf16 values; fp32 rows take a second term (22 bits).
 // With v's scale inside the exponent, w_j = 2^(s_j log2 e + log2 vs_j - M), the sum of w V needs no scale and the sum of
 // weights is that of w_j / vs_j (a page of zeros has vs = 2^-126: kPgaLeastV).  w is rounded to fp16 (11 bits; a second term for fp32 rows), at up to 2^15 so that small ones keep them.  Sums are fp32.
-// M only moves when a score exceeds it by more than 6, so the sums are rarely rescaled.
+// M only moves when a score exceeds it by more than 6, so the sums are rarely rescaled (all rows of a warp with one that needs it).
 // Sequences that span CTAs are put together by k_pages_attn_join from the partial results, in fixed order.
 //
-// Measured (B200): 96 sequences of 256 - 4096 tokens, 12 heads of 64, one row: 71 us with the join for 321 MB, 4.5 TB/s, 0.69 of the
-// measured copy rate.  Four sequences of 65537 - 262144 tokens, 14 / 2 heads: 44 us for 168 MB (25.6 at the copy rate).  Parts of equal length instead of
+// Measured (B200, replayed from a graph): 96 sequences of 256 - 4096 tokens, 12 heads of 64, one row: 72 us with the join for 321 MB, 4.45 TB/s,
+// 0.68 of the measured copy rate; 8 KV heads of 128, 4 rows each, 114 us for 429 MB, 3.8 TB/s (168 registers: two CTAs an SM).  fp32 rows in
+// number, 2 x 1024 against 2111 - 4096 tokens, 32 / 8 heads of 128: 956 us, 83 TFLOP/s (tiles of 64 rows, two terms of q and of the weights).  Four sequences of 65537 - 262144 tokens, 14 / 2 heads: 44 us for 168 MB (25.6 at the copy rate).  Parts of equal length instead of
 // equal cost, at an earlier state: 110 and 77 us against 105 and 49 (the parallel join came with it).
 #pragma once
 #include "pages_kernels.cuh"

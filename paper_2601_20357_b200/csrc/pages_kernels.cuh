@@ -150,7 +150,7 @@ __device__ __forceinline__ void open8(const Raw8<float>& r, float (&f)[8]) {
 // tokens of the block) is worked by TPU threads, each with up to MAXI items of 8 rotated pairs in registers between the
 // block's maximum and the rounding: k, v and q are read once, the next unit's while this one is worked.  Short units (single
 // tokens) take a warp each, 8 at once; long ones the whole CTA, of 256 or 512 threads: an item a thread keeps most warps on an SM (64
-// tokens of 128 values: two items on 256 threads 144 us, one on 512 112 us, at 18,800 tokens of 48 heads).
+// tokens of 128 values: two items on 256 threads 144 us, one on 512 113 us, 424 MB, at 18,800 tokens of 48 heads; fp32 156 us, 809 MB, 5.2 TB/s).
 template <typename T, int TPU, int MAXI>
 __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 && MAXI == 1 ? 2 : 1) k_pages_append(const AppendArgs A) {
   extern __shared__ float4 ap_cs[];               // [4][items] cosine and sine of two frequencies: the lanes' places are neighbours
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(TPU == 32 ? kAppendThreads : TPU, TPU == 512 &
 }
 
 // The other way: the first `len` tokens of a sequence into a dense cache row [L][Hkv][cap][hd] (a code times a power of two is a bf16 value
-// already).  Blocks without a page become zeros.  grid (ceil(len / page_tokens), 2 Hkv, L)
+// already).  Blocks without a page become zeros.  Measured: 4 layers of 12 heads of 64, 704 tokens 8.2 us, 8192 32 us (151 MB, 4.7 TB/s).  grid (ceil(len / page_tokens), 2 Hkv, L)
 template <typename T>
 __global__ void __launch_bounds__(128) k_pages_load_row(const PagesDev P, int seq, int len, T* __restrict__ k, T* __restrict__ v, int cap, int* kv_len) {
   const int b = blockIdx.x, head = blockIdx.y >> 1, layer = blockIdx.z, hd = P.hd, tid = threadIdx.x;

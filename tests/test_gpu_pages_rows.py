@@ -53,3 +53,15 @@ def test_long_sequences_of_blocks_span_ctas(rows):
         p.attention(0, q, outs[-1], T.ints([0]), T.ints([0, rows]), T.ints([9000]), rows, scale=0.125)
     p.attention(0, q, q, T.ints([0]), T.ints([0, rows]), T.ints([9000]), rows, scale=0.125)       # in place
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and torch.equal(outs[0], q) and p.last_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("max_new", [9, 40, 100, 1000])
+def test_more_rows_announced_than_any_entry_has(max_new, dtype):
+    """max_new chooses kernel and tile; most of a tile is then empty."""
+    length, counts = [1, 200, 333, 0, 64], [1, 3, 0, 2, 1]
+    c = T.make(length, Hkv=2, ps=64, hd=64, seed=5, nan_tail=True)
+    p = T.to_gpu(c)
+    first = (1 + np.concatenate([[0], np.cumsum(counts)])).tolist()
+    T.check_attention(c, p, 1, T.queries(first[-1] + 2, 4, 64, 9), first, length, dtype=dtype, max_new=max_new)
+    assert p.last_error() == 0
